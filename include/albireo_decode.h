@@ -1,0 +1,129 @@
+/*
+ * albireo_decode.h -- C ABI of the operators between a decode step's last hidden states and the logits
+ * the sampling entry points of albireo.h take.
+ *
+ * A decode step ends with the residual addition and norm of the newest hidden state of every sequence,
+ * the language-model head (one product with the [vocabulary, width] weights), and the changes a request
+ * asks for on its logits before they are sampled: biases, penalties, a grammar's mask.  The paper's
+ * sampling task starts at the logits these produce (sec. 2.1; the features of sec. 8.1).
+ *
+ *   albireo_rms_norm       residual addition and root-mean-square norm, in the input's type and / or in
+ *                          8 bits with a scale per row
+ *   albireo_matmul_w4      product of bf16 or 8-bit rows with 4-bit weights and group scales
+ *   albireo_adjust_logits  biases, penalties and grammar masks on the logits
+ *
+ * The conventions are albireo.h's: array arguments are DEVICE pointers unless marked [host], the caller
+ * owns every buffer, all work is enqueued on `stream`, nothing synchronises or allocates, host-checkable
+ * problems return a status and enqueue nothing, and results are bit-identical from run to run.  These
+ * entry points need no workspace.  Pointers must be aligned to their element size, strides are in
+ * elements of the array, and an output overlaps an input only where the entry point says so.
+ */
+#ifndef ALBIREO_DECODE_H
+#define ALBIREO_DECODE_H
+
+#include "albireo.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Widest row albireo_rms_norm takes. */
+#define ALBIREO_MAX_NORM_WIDTH 32768
+
+/*
+ * Residual addition and root-mean-square norm of T rows of D values:
+ *     h = x + residual                          (h = x when residual is NULL)
+ *     y = (h * rstd) * weight,  rstd = 1 / sqrt(mean(h^2) + eps)      (weight NULL: all ones)
+ *     amax = max |y|,  scale = amax / 127,  q = round-half-even(y * (127 / amax))
+ * in 32 bits; each output is rounded once from them.  The mean is taken of the unrounded sums h.  A row
+ * whose sum of squares leaves the range of 32 bits is summed in 64.
+ *   x, residual    [T, ldx], [T, ldr] of `dtype`
+ *   weight         [D] of `weight_dtype`
+ *   out_residual   [T, ldro] of `dtype`: h, or NULL.  May be x or residual themselves (same stride).
+ *   out            [T, ldo] of `dtype`: y, or NULL.  May be x or residual themselves (same stride), when
+ *                  out_residual is not that array too.
+ *   out_q          [T, ldq] int8 and out_scale [T] fp32: the 8-bit form (y ~ q * scale), or both NULL
+ * At least one output is given.  A row with amax below 2^-120 (all zeros) has scale 0 and q 0; a row
+ * holding a NaN or an infinity has scale NaN and q 0 (its y: as the formula gives it).
+ */
+albireo_status_t albireo_rms_norm(const void* x, albireo_dtype_t dtype, int64_t T, int64_t D, int64_t ldx,
+                                  const void* residual, int64_t ldr, const void* weight,
+                                  albireo_dtype_t weight_dtype, float eps, void* out_residual, int64_t ldro,
+                                  void* out, int64_t ldo, int8_t* out_q, int64_t ldq, float* out_scale,
+                                  hipStream_t stream);
+
+/* Types of the rows albireo_matmul_w4 multiplies. */
+typedef enum { ALBIREO_ROWS_BF16 = 1, ALBIREO_ROWS_I8 = 2 } albireo_rows_t;
+
+/*
+ * 4-bit weights [N, K] (host struct of device arrays, read during a call only): N outputs over K inputs,
+ *     W[n, k] = scales[n, k / group] * (q[n, k] - zeros[n, k / group])
+ * with q in 0 .. 15, two to a byte: column k in byte k / 2 of its row, an even k in the low four bits.
+ */
+typedef struct {
+  int64_t N, K;                 /* [host values] K a multiple of group                             */
+  int32_t group;                /* [host value] columns per scale: 32, 64 or 128                   */
+  const uint8_t* q;             /* [N, ldq] packed columns, ldq >= K / 2 bytes                     */
+  int64_t ldq;
+  const void* scales;           /* [N, lds] of scale_dtype, lds >= K / group                       */
+  albireo_dtype_t scale_dtype;
+  int64_t lds;
+  const uint8_t* zeros;         /* [N, ldz] zero points, ldz >= K / group, or NULL: 8 everywhere   */
+  int64_t ldz;
+} albireo_w4_t;
+
+/*
+ * out[b, n] = x_scale[b] * sum_k x[b, k] * W[n, k]
+ *   x          [B, ldx] bf16 (ALBIREO_ROWS_BF16; x_scale must be NULL) or int8 (ALBIREO_ROWS_I8)
+ *   x_scale    [B] fp32 scales of int8 rows (albireo_rms_norm's out_scale)
+ *   out        [B, ldo] of out_dtype, ldo >= N
+ * Sums are held in 32 bits: integers within a group of int8 rows (exact), fp32 else; the result is rounded
+ * once to out_dtype.  Their order depends on the shape, B included.  A NaN or an infinity in a row of x, or
+ * in a scale, makes the outputs it enters non-finite.
+ */
+albireo_status_t albireo_matmul_w4(const void* x, albireo_rows_t x_type, int64_t B, int64_t ldx,
+                                   const float* x_scale, const albireo_w4_t* weight, void* out,
+                                   albireo_dtype_t out_dtype, int64_t ldo, hipStream_t stream);
+
+/*
+ * What requests ask of their logits beside penalties (host struct, read during the call only; every
+ * pointer is a device array).
+ */
+typedef struct {
+  /* Additive biases, CSR as the histories are: row i's are entries bias_offsets[i] .. bias_offsets[i + 1].
+   * An id that occurs more than once in a row takes its last entry. */
+  const int64_t* bias_offsets;  /* [B+1], or NULL: no biases                                       */
+  const int32_t* bias_ids;      /* [bias_len] token ids; ids outside [0, V) are skipped + flagged  */
+  const float* bias_values;     /* [bias_len]; -inf bans its token; NaN counts as 0 + flagged      */
+  int64_t bias_len;             /* [host value]                                                    */
+  /* Grammar masks: bit v % 32 of word v / 32 set lets token v through. */
+  const uint32_t* mask;         /* [mask_rows, mask_ld] words, mask_ld >= ceil(V / 32), or NULL    */
+  int64_t mask_rows, mask_ld;   /* [host values]                                                   */
+  const int32_t* mask_index;    /* [B] the mask row of each row, negative: none; NULL: row i has mask i */
+} albireo_constraints_t;
+
+/*
+ * Change the logits as their requests ask, in this order:
+ *   1. x + bias (fp32), where the row has a bias for the token;
+ *   2. the penalties of albireo.h's step 2, as albireo_apply_penalties takes them from params;
+ *   3. -inf where the row's mask bit is clear, whatever the logit was (a NaN included).
+ * A row whose mask lets nothing through comes out as -inf throughout (albireo_sample: id -1, EMPTY).
+ * albireo_sample on the result without penalties draws what albireo_sample draws with them on the fp32
+ * result of the biases and masks alone.
+ *   params       [host] penalties and histories as albireo_apply_penalties; NULL: no penalties
+ *   constraints  [host] or NULL: neither biases nor masks
+ *   out          [B, ldo] of out_dtype, ldo >= V.  It may be `logits` itself when out_dtype is dtype and
+ *                ldo is ld: then only what changes is written.
+ *   out_flags    [B] or NULL: ALBIREO_FLAG_BAD_INPUT for an id outside [0, V), ALBIREO_FLAG_BAD_PARAM for a
+ *                malformed penalty, a NaN bias, bad offsets (their list is left out) or a mask_index past
+ *                mask_rows (no mask); and the penalty state's flags
+ */
+albireo_status_t albireo_adjust_logits(const void* logits, albireo_dtype_t dtype, int64_t B, int64_t V, int64_t ld,
+                                       const albireo_params_t* params, const albireo_constraints_t* constraints,
+                                       void* out, albireo_dtype_t out_dtype, int64_t ldo, uint32_t* out_flags,
+                                       hipStream_t stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* ALBIREO_DECODE_H */

@@ -556,3 +556,6 @@ def raw_call(name: str):
 
 
 Params = _Params
+
+from .decode import (DECODE_EXPORTED, MAX_NORM_WIDTH, Constraints, NormOut, PreparedAdjust, PreparedMatmulW4,  # noqa: E402
+                     PreparedNorm, W4Weight, adjust_logits, matmul_w4, rms_norm)

@@ -1,0 +1,270 @@
+"""Binding of the operators ahead of the sampler (``include/albireo_decode.h``): the norm of the last hidden
+states, the 4-bit language-model head, and the changes requests ask for on their logits.
+
+Argument marshalling only, as in the package itself, which re-exports every public name.  Each operator has a
+function and a prepared form: an object that holds its arguments marshalled once, for a decode loop whose
+buffers stay in place; calling it enqueues the operator on its stream (the current one by default).
+"""
+from __future__ import annotations
+
+import ctypes
+import dataclasses
+from typing import Optional
+
+import torch
+
+from . import (BF16, F32, OK, AlbireoError, SamplingParams, _lib, _Params, _params, _rows, _stream, _vp, _i32, _i64)
+
+ROWS_BF16, ROWS_I8 = 1, 2
+MAX_NORM_WIDTH = 32768
+
+
+class _W4(ctypes.Structure):
+    _fields_ = [("N", _i64), ("K", _i64), ("group", _i32), ("q", _vp), ("ldq", _i64), ("scales", _vp),
+                ("scale_dtype", ctypes.c_int), ("lds", _i64), ("zeros", _vp), ("ldz", _i64)]
+
+
+class _Constraints(ctypes.Structure):
+    _fields_ = [("bias_offsets", _vp), ("bias_ids", _vp), ("bias_values", _vp), ("bias_len", _i64), ("mask", _vp),
+                ("mask_rows", _i64), ("mask_ld", _i64), ("mask_index", _vp)]
+
+
+_lib.albireo_rms_norm.argtypes = [_vp, ctypes.c_int, _i64, _i64, _i64, _vp, _i64, _vp, ctypes.c_int, ctypes.c_float,
+                                  _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]
+_lib.albireo_rms_norm.restype = ctypes.c_int
+_lib.albireo_matmul_w4.argtypes = [_vp, ctypes.c_int, _i64, _i64, _vp, ctypes.POINTER(_W4), _vp, ctypes.c_int, _i64,
+                                   _vp]
+_lib.albireo_matmul_w4.restype = ctypes.c_int
+_lib.albireo_adjust_logits.argtypes = [_vp, ctypes.c_int, _i64, _i64, _i64, ctypes.POINTER(_Params),
+                                       ctypes.POINTER(_Constraints), _vp, ctypes.c_int, _i64, _vp, _vp]
+_lib.albireo_adjust_logits.restype = ctypes.c_int
+
+DECODE_EXPORTED = ("albireo_rms_norm", "albireo_matmul_w4", "albireo_adjust_logits")
+
+_CODE = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _code(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in _CODE:
+        raise ValueError("%s must be bfloat16 or float32" % name)
+    return _CODE[t.dtype]
+
+
+def _matrix(t: torch.Tensor, name: str, device, dtype, rows: int, cols: int) -> int:
+    """Check a 2-D array with unit stride along its rows; returns its row stride."""
+    if t.device != device or t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols \
+            or (cols > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be a %s tensor [%d, %d] on %s with unit stride along its rows"
+                         % (name, dtype, rows, cols, device))
+    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def _vector(t: torch.Tensor, name: str, device, dtype, n: int) -> int:
+    if t.device != device or t.dtype != dtype or t.dim() != 1 or t.shape[0] < n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor [%d] on %s" % (name, dtype, n, device))
+    return t.data_ptr()
+
+
+class _Prepared:
+    """The marshalled arguments of one call.  ``result`` is what the function of the same name returns."""
+    _name = ""
+
+    def _set(self, args, keep, result, stream):
+        self._fn = getattr(_lib, self._name)
+        self._args, self._keep, self.result, self.stream = args, keep, result, stream
+
+    def __call__(self):
+        st = self._fn(*self._args, _stream(self.stream))
+        if st != OK:
+            raise AlbireoError(st, self._name)
+        return self.result
+
+
+# --------------------------------------------------------------------------------------------------
+# albireo_rms_norm
+# --------------------------------------------------------------------------------------------------
+@dataclasses.dataclass
+class NormOut:
+    """Outputs of rms_norm: the normed rows, the residual stream, the 8-bit rows and their scales (None where
+    not asked for)."""
+    y: Optional[torch.Tensor] = None         # [T, D] as x
+    residual: Optional[torch.Tensor] = None  # [T, D] as x
+    q: Optional[torch.Tensor] = None         # [T, D] int8
+    scale: Optional[torch.Tensor] = None     # [T] float32
+
+
+class PreparedNorm(_Prepared):
+    """rms_norm with its arguments marshalled once; calling it enqueues the launch and returns ``out``."""
+    _name = "albireo_rms_norm"
+
+    def __init__(self, x, weight=None, eps: float = 1e-6, residual=None, normed: bool = True, quant: bool = False,
+                 out: Optional[NormOut] = None, stream=None):
+        if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+            raise ValueError("x must be a 2-D tensor with unit stride along its rows")
+        dt, dev, (T, D) = _code(x, "x"), x.device, x.shape
+        ldx = x.stride(0) if T > 1 else max(D, x.stride(0))
+        wcode = F32 if weight is None else _code(weight, "weight")
+        wptr = None if weight is None else _vector(weight, "weight", dev, weight.dtype, D)
+        ldr = 0 if residual is None else _matrix(residual, "residual", dev, x.dtype, T, D)
+        if out is None:
+            out = NormOut(y=torch.empty((T, D), dtype=x.dtype, device=dev) if normed else None,
+                          residual=torch.empty((T, D), dtype=x.dtype, device=dev) if residual is not None else None,
+                          q=torch.empty((T, D), dtype=torch.int8, device=dev) if quant else None,
+                          scale=torch.empty(T, dtype=torch.float32, device=dev) if quant else None)
+        elif (out.y is not None) != normed or (out.q is not None) != quant or (out.scale is not None) != quant:
+            raise ValueError("out must hold y when normed, and q and scale when quant")
+        ldo = 0 if out.y is None else _matrix(out.y, "out.y", dev, x.dtype, T, D)
+        ldro = 0 if out.residual is None else _matrix(out.residual, "out.residual", dev, x.dtype, T, D)
+        ldq = 0 if out.q is None else _matrix(out.q, "out.q", dev, torch.int8, T, D)
+        sptr = None if out.scale is None else _vector(out.scale, "out.scale", dev, torch.float32, T)
+        self._set((x.data_ptr(), dt, T, D, ldx, None if residual is None else residual.data_ptr(), ldr, wptr, wcode, eps,
+                   None if out.residual is None else out.residual.data_ptr(), ldro,
+                   None if out.y is None else out.y.data_ptr(), ldo,
+                   None if out.q is None else out.q.data_ptr(), ldq, sptr), (x, weight, residual), out, stream)
+
+
+def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+             residual: Optional[torch.Tensor] = None, normed: bool = True, quant: bool = False,
+             out: Optional[NormOut] = None, stream=None) -> NormOut:
+    """albireo_rms_norm: the root-mean-square norm of the rows of x [T, D] (of x + residual), times weight [D].
+
+    normed asks for the rows in x's type, quant for int8 rows with float32 scales; with a residual the sum is
+    returned too.  ``out`` gives the buffers (out.residual may be the residual itself: in place)."""
+    return PreparedNorm(x, weight, eps, residual, normed, quant, out, stream)()
+
+
+# --------------------------------------------------------------------------------------------------
+# albireo_matmul_w4
+# --------------------------------------------------------------------------------------------------
+@dataclasses.dataclass
+class W4Weight:
+    """4-bit weights: W[n, k] = scales[n, k // group] * (q[n, k] - zeros[n, k // group]), the group of 32, 64 or
+    128 columns following from the shapes; zeros None stands for 8."""
+    q: torch.Tensor                        # uint8 [N, K / 2], the even column in the low four bits
+    scales: torch.Tensor                   # bfloat16 or float32 [N, K / group]
+    zeros: Optional[torch.Tensor] = None   # uint8 [N, K / group]
+
+    def __post_init__(self):
+        if self.q.dim() != 2 or self.scales.dim() != 2 or self.scales.shape[1] < 1:
+            raise ValueError("q and scales must be 2-D tensors")
+        N, K, G = self.q.shape[0], 2 * self.q.shape[1], self.scales.shape[1]
+        if K % G or K // G not in (32, 64, 128):
+            raise ValueError("scales must hold one value per 32, 64 or 128 columns")
+        self.N, self.K, self.group = N, K, K // G
+        self.struct = _W4(N=N, K=K, group=self.group)
+        dev = self.q.device
+        self.struct.ldq = _matrix(self.q, "q", dev, torch.uint8, N, K // 2)
+        self.struct.scale_dtype = _code(self.scales, "scales")
+        self.struct.lds = _matrix(self.scales, "scales", dev, self.scales.dtype, N, G)
+        self.struct.q, self.struct.scales = self.q.data_ptr(), self.scales.data_ptr()
+        if self.zeros is not None:
+            self.struct.ldz = _matrix(self.zeros, "zeros", dev, torch.uint8, N, G)
+            self.struct.zeros = self.zeros.data_ptr()
+
+
+class PreparedMatmulW4(_Prepared):
+    """matmul_w4 with its arguments marshalled once; calling it enqueues the product and returns ``out``."""
+    _name = "albireo_matmul_w4"
+
+    def __init__(self, x, weight: W4Weight, x_scale=None, out=None, out_dtype: torch.dtype = torch.float32, stream=None):
+        if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1) or x.shape[1] != weight.K:
+            raise ValueError("x must be a 2-D tensor [B, %d] with unit stride along its rows" % weight.K)
+        if x.dtype not in (torch.bfloat16, torch.int8):
+            raise ValueError("x must be bfloat16 or int8")
+        i8 = x.dtype == torch.int8
+        if i8 != (x_scale is not None):
+            raise ValueError("x_scale goes with int8 rows")
+        dev, B = x.device, x.shape[0]
+        if weight.q.device != dev:
+            raise ValueError("the weights live on %s, not %s" % (weight.q.device, dev))
+        sptr = _vector(x_scale, "x_scale", dev, torch.float32, B) if i8 else None
+        if out is None:
+            out = torch.empty((B, weight.N), dtype=out_dtype, device=dev)
+        code = _code(out, "out")
+        ldo = _matrix(out, "out", dev, out.dtype, B, weight.N)
+        ldx = x.stride(0) if B > 1 else max(weight.K, x.stride(0))
+        self._set((x.data_ptr(), ROWS_I8 if i8 else ROWS_BF16, B, ldx, sptr, ctypes.byref(weight.struct),
+                   out.data_ptr(), code, ldo), (x, x_scale, weight), out, stream)
+
+
+def matmul_w4(x: torch.Tensor, weight: W4Weight, x_scale: Optional[torch.Tensor] = None, out=None,
+              out_dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
+    """albireo_matmul_w4: x [B, K] (bfloat16, or int8 with float32 x_scale [B]) times the 4-bit weights
+    [N, K] transposed; [B, N] in out's type, or out_dtype."""
+    return PreparedMatmulW4(x, weight, x_scale, out, out_dtype, stream)()
+
+
+# --------------------------------------------------------------------------------------------------
+# albireo_adjust_logits
+# --------------------------------------------------------------------------------------------------
+@dataclasses.dataclass
+class Constraints:
+    """Biases and grammar masks of a batch as device tensors (None turns one off)."""
+    bias_offsets: Optional[torch.Tensor] = None  # int64 [B + 1]
+    bias_ids: Optional[torch.Tensor] = None      # int32
+    bias_values: Optional[torch.Tensor] = None   # float32
+    mask: Optional[torch.Tensor] = None          # int32 [rows, ceil(V / 32)] bit words (uint32 bit patterns)
+    mask_index: Optional[torch.Tensor] = None    # int32 [B] mask row, negative: none; None: row i has mask i
+
+
+def _constraints(c: Optional[Constraints], B: int, V: int, device) -> Optional[_Constraints]:
+    if c is None:
+        return None
+    s = _Constraints()
+    if c.bias_offsets is not None:
+        if c.bias_ids is None or c.bias_values is None or c.bias_ids.numel() != c.bias_values.numel():
+            raise ValueError("bias_offsets needs bias_ids and bias_values of one length")
+        n = c.bias_ids.numel()
+        s.bias_offsets = _vector(c.bias_offsets, "bias_offsets", device, torch.int64, B + 1)
+        s.bias_ids = _vector(c.bias_ids, "bias_ids", device, torch.int32, n)
+        s.bias_values = _vector(c.bias_values, "bias_values", device, torch.float32, n)
+        s.bias_len = n
+    if c.mask is not None:
+        if c.mask.dim() != 2 or c.mask.shape[1] < (V + 31) // 32:
+            raise ValueError("mask must be a 2-D tensor with at least %d words a row" % ((V + 31) // 32))
+        s.mask_ld = _matrix(c.mask, "mask", device, torch.int32, *c.mask.shape)
+        s.mask, s.mask_rows = c.mask.data_ptr(), c.mask.shape[0]
+        if c.mask_index is not None:
+            s.mask_index = _vector(c.mask_index, "mask_index", device, torch.int32, B)
+            if c.mask.shape[0] == 0:
+                s.mask = s.mask_index  # an empty tensor has no address; a mask of no rows is never read
+        elif c.mask.shape[0] < B:
+            raise ValueError("mask needs a row for each row of logits, or a mask_index")
+    return s
+
+
+class PreparedAdjust(_Prepared):
+    """adjust_logits with its arguments marshalled once; calling it enqueues the launch and returns
+    (out, flags)."""
+    _name = "albireo_adjust_logits"
+
+    def __init__(self, logits, params: Optional[SamplingParams] = None, constraints: Optional[Constraints] = None,
+                 V: Optional[int] = None, out=None, out_dtype: torch.dtype = torch.float32, flags=None, stream=None):
+        dev = logits.device
+        B, V, ld = _rows(logits, V)
+        dt = _code(logits, "logits")
+        if out is None:
+            out = torch.empty((B, V), dtype=out_dtype, device=dev)
+        code = _code(out, "out")
+        if out.data_ptr() == logits.data_ptr() and out.shape == logits.shape:
+            ldo = ld  # in place, padding columns past V included in the shape
+            if out.device != dev or out.dtype != logits.dtype or out.stride() != logits.stride():
+                raise ValueError("an out in place of the logits must have their type and strides")
+        else:
+            ldo = _matrix(out, "out", dev, out.dtype, B, V)
+        if flags is None:
+            flags = torch.empty(B, dtype=torch.int32, device=dev)
+        prm = _params(params, dev)
+        con = _constraints(constraints, B, V, dev)
+        self._set((logits.data_ptr(), dt, B, V, ld, ctypes.byref(prm) if prm else None,
+                   ctypes.byref(con) if con else None, out.data_ptr(), code, ldo,
+                   _vector(flags, "flags", dev, torch.int32, B)), (logits, params, constraints, prm, con),
+                  (out, flags), stream)
+
+
+def adjust_logits(logits: torch.Tensor, params: Optional[SamplingParams] = None,
+                  constraints: Optional[Constraints] = None, V: Optional[int] = None, out=None,
+                  out_dtype: torch.dtype = torch.float32, flags=None, stream=None):
+    """albireo_adjust_logits: biases, then penalties, then grammar masks on the logits [B, V].  Returns (out,
+    flags int32 [B]); out=logits changes them in place, writing only what changes."""
+    return PreparedAdjust(logits, params, constraints, V, out, out_dtype, flags, stream)()
