@@ -34,7 +34,7 @@ extern "C" {
  * Residual addition and root-mean-square norm of T rows of D values:
  *     h = x + residual                          (h = x when residual is NULL)
  *     y = (h * rstd) * weight,  rstd = 1 / sqrt(mean(h^2) + eps)      (weight NULL: all ones)
- *     amax = max |y|,  scale = amax / 127,  q = round-half-even(y * (127 / amax))
+ *     amax = max |y|,  scale = amax / 127,  q = round-half-even(y * (127 * (1 / amax)))
  * in 32 bits; each output is rounded once from them.  The mean is taken of the unrounded sums h.  A row
  * whose sum of squares leaves the range of 32 bits is summed in 64.
  *   x, residual    [T, ldx], [T, ldr] of `dtype`

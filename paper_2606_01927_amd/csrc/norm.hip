@@ -4,7 +4,6 @@
 
 #include <math.h>
 #include <stdint.h>
-#include <string.h>
 
 #include <utility>
 
@@ -23,56 +22,201 @@ struct NormArgs {
   unsigned char* out;
   int8_t* out_q;
   float* out_scale;
-  int64_t ldx, ldr, ldro, ldo, ldq;
+  int64_t T, ldx, ldr, ldro, ldo, ldq;
   int32_t D;
   float eps;
 };
 
-constexpr int NORM_NT = 256;
+// N consecutive values of a row as they lie in memory, at an address aligned to the element only (gfx950
+// takes unaligned vector accesses).
+template <class DT, int N>
+struct Values {
+  static constexpr int DW = N * DT::ES / 4;
+  uint32_t d[DW];
+  __device__ __forceinline__ void load(const unsigned char* p) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+    if constexpr (DW == 2) {
+      const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+      d[0] = v.x, d[1] = v.y;
+    } else {
+#pragma unroll
+      for (int g = 0; g < DW / 4; ++g) {
+        const u32x4 v = reinterpret_cast<const u32x4*>(p)[g];
+        d[4 * g] = v.x, d[4 * g + 1] = v.y, d[4 * g + 2] = v.z, d[4 * g + 3] = v.w;
+      }
+    }
+  }
+  __device__ __forceinline__ float get(int e) const {
+    if constexpr (DT::ES == 4) return __uint_as_float(d[e]);
+    else return __uint_as_float((e & 1) ? d[e / 2] & 0xffff0000u : d[e / 2] << 16);
+  }
+};
 
-// One workgroup per row, three passes over it.
-template <class DT, class WT>
-__global__ __launch_bounds__(NORM_NT) void k_norm(NormArgs a) {
-  __shared__ float h[ALBIREO_MAX_NORM_WIDTH];
-  __shared__ double red[NORM_NT / 64];
-  __shared__ float redm[NORM_NT / 64];
-  const int t = threadIdx.x;
-  const int64_t row = blockIdx.x;
-  const unsigned char* xr = a.x + row * a.ldx * DT::ES;
-  const unsigned char* rr = a.residual ? a.residual + row * a.ldr * DT::ES : nullptr;
-  double ss = 0.0;
-  for (int i = t; i < a.D; i += NORM_NT) {
-    float v = DT::load1(xr, i);
-    if (rr) v += DT::load1(rr, i);
-    h[i] = v;
-    ss += (double)v * (double)v;
+template <class DT, int N>
+__device__ __forceinline__ void store_values(unsigned char* p, const float (&v)[N]) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+  if constexpr (DT::ES == 2) {
+    static_assert(N == 8, "a slot");
+    *reinterpret_cast<u32x4*>(p) =
+        u32x4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+  } else {
+    static_assert(N == 4, "a slot");
+    *reinterpret_cast<u32x4*>(p) =
+        u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
   }
-  for (int d = 32; d; d >>= 1) ss += __shfl_xor(ss, d);
-  if (lane_id() == 0) red[wave_id()] = ss;
-  __syncthreads();
-  ss = ((red[0] + red[1]) + red[2]) + red[3];
-  const float rstd = (float)(1.0 / sqrt(ss / a.D + (double)a.eps));
-  float amax = 0.0f;
-  bool bad = !isfinite(ss);
-  for (int i = t; i < a.D; i += NORM_NT) {
-    const float w = a.weight ? WT::load1(a.weight, i) : 1.0f;
-    const float y = h[i] * rstd * w;
-    if (a.out_residual) store1<DT>(a.out_residual + row * a.ldro * DT::ES, i, h[i]);
-    if (a.out) store1<DT>(a.out + row * a.ldo * DT::ES, i, y);
-    bad |= !isfinite(y);
-    amax = fmaxf(amax, fabsf(y));
-    h[i] = y;
+}
+
+__device__ __forceinline__ uint32_t q_byte(float v) { return (uint32_t)(int)rintf(v) & 0xffu; }
+
+// sum of a double over the wave's lanes, combined in the order of wave_sum
+__device__ __forceinline__ double wave_sum_d(double v) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+// A row is held in registers by TPR threads, SPT slots of 16 bytes of its type each (8 bf16 or 4 fp32): 64
+// threads (a wave, without a barrier) for short rows, else a workgroup of 256 or 1024.  Every input is read
+// once and every output written once; the loads of a row all go out before the first is used (a slot past the
+// row's last reloads that one and counts as zeros).  Rows need no alignment past the element's, so odd widths
+// and strides keep the wide accesses; the values behind the last whole slot are one each for the first threads.
+//
+// The squares are added in double; mean, root and reciprocal are fp32 operations on the rounded sum.  An fp32
+// sum of a row's thousands of squares is off by a unit or two, and with it would be whether an 8-bit value
+// next to the middle of two steps goes up or down.  A sum that leaves fp32 stays in double.
+//
+// Bound: HBM.
+template <class DT, class WT, int TPR, int SPT>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormArgs a) {
+  constexpr int VEC = DT::VEC, ES = DT::ES, NW = TPR / 64;
+  __shared__ double red[NW];
+  __shared__ int redm[NW];
+  const int t = TPR == 64 ? lane_id() : (int)threadIdx.x;
+  const int64_t row = TPR == 64 ? (int64_t)blockIdx.x * 4 + wave_id() : (int64_t)blockIdx.x;
+  if (TPR == 64 && row >= a.T) return;
+  const unsigned char* xr = a.x + row * a.ldx * ES;
+  const unsigned char* rr = a.residual + row * a.ldr * ES;
+  const int full = a.D / VEC, rest = a.D - full * VEC;
+  const bool has_res = a.residual != nullptr, has_w = a.weight != nullptr;
+
+  Values<DT, VEC> x[SPT], r[SPT];
+  Values<WT, VEC> w[SPT];
+  if (full) {
+#pragma unroll
+    for (int s = 0; s < SPT; ++s) x[s].load(xr + min(s * TPR + t, full - 1) * 16);
+    if (has_res) {
+#pragma unroll
+      for (int s = 0; s < SPT; ++s) r[s].load(rr + min(s * TPR + t, full - 1) * 16);
+    }
+    if (has_w) {
+#pragma unroll
+      for (int s = 0; s < SPT; ++s) w[s].load(a.weight + min(s * TPR + t, full - 1) * (VEC * WT::ES));
+    }
   }
+  float he = 0.0f, we = 1.0f;  // value full * VEC + t
+  if (t < rest) {
+    he = DT::load1(xr, full * VEC + t);
+    if (has_res) he += DT::load1(rr, full * VEC + t);
+    if (has_w) we = WT::load1(a.weight, full * VEC + t);
+  }
+  float h[SPT][VEC];
+  double ss = (double)he * (double)he;
+#pragma unroll
+  for (int s = 0; s < SPT; ++s) {
+    const bool in = s * TPR + t < full;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      float v = x[s].get(e);
+      if (has_res) v += r[s].get(e);
+      h[s][e] = in ? v : 0.0f;
+      ss = fma((double)h[s][e], (double)h[s][e], ss);
+    }
+    if (a.out_residual && in) store_values<DT>(a.out_residual + (row * a.ldro + (s * TPR + t) * VEC) * ES, h[s]);
+  }
+  if (a.out_residual && t < rest) store1<DT>(a.out_residual + row * a.ldro * ES, full * VEC + t, he);
+  ss = wave_sum_d(ss);
+  if constexpr (NW > 1) {
+    if (lane_id() == 0) red[wave_id()] = ss;
+    __syncthreads();
+    ss = red[0];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) ss += red[i];
+  }
+  float rstd;
+  const float sum = (float)ss;
+  if (isinf(sum)) rstd = (float)(1.0 / sqrt(ss / a.D + (double)a.eps));
+  else rstd = 1.0f / sqrtf(sum * (1.0f / (float)a.D) + a.eps);
+
+  int top = 0;  // the largest |y| as its bits: a NaN or an infinity is above every number
+  he = (he * rstd) * we;
+  if (t < rest) top = (int)(__float_as_uint(he) & 0x7fffffffu);
+#pragma unroll
+  for (int s = 0; s < SPT; ++s) {
+    const bool in = s * TPR + t < full;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      h[s][e] *= rstd;
+      if (has_w) h[s][e] *= w[s].get(e);
+      top = max(top, in ? (int)(__float_as_uint(h[s][e]) & 0x7fffffffu) : 0);
+    }
+    if (a.out && in) store_values<DT>(a.out + (row * a.ldo + (s * TPR + t) * VEC) * ES, h[s]);
+  }
+  if (a.out && t < rest) store1<DT>(a.out + row * a.ldo * ES, full * VEC + t, he);
   if (!a.out_q) return;
-  amax = wave_max(amax);
-  if (lane_id() == 0) redm[wave_id()] = amax;
-  bad = __syncthreads_or(bad);
-  amax = fmaxf(fmaxf(redm[0], redm[1]), fmaxf(redm[2], redm[3]));
-  const bool zero = bad || amax < 0x1p-120f;
-  const float inv = zero ? 0.0f : 127.0f / amax;
-  for (int i = t; i < a.D; i += NORM_NT) a.out_q[row * a.ldq + i] = zero ? 0 : (int8_t)(int)rintf(h[i] * inv);
+  top = wave_max_i(top);
+  if constexpr (NW > 1) {
+    if (lane_id() == 0) redm[wave_id()] = top;
+    __syncthreads();
+    top = redm[0];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) top = max(top, redm[i]);
+  }
+  const float amax = __uint_as_float((uint32_t)top);
+  const bool bad = top >= 0x7f800000, zero = bad || amax < 0x1p-120f;
+  const float inv = zero ? 0.0f : 127.0f * (1.0f / amax);
+  int8_t* qr = a.out_q + row * a.ldq;
+#pragma unroll
+  for (int s = 0; s < SPT; ++s) {
+    uint32_t p[VEC / 4];
+#pragma unroll
+    for (int g = 0; g < VEC / 4; ++g) {
+      const float* v = &h[s][4 * g];
+      p[g] = q_byte(v[0] * inv) | q_byte(v[1] * inv) << 8 | q_byte(v[2] * inv) << 16 | q_byte(v[3] * inv) << 24;
+      if (zero) p[g] = 0;
+    }
+    if (s * TPR + t < full) {
+      typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(1)));
+      typedef uint32_t u32x1 __attribute__((aligned(1)));
+      if constexpr (VEC == 4) *reinterpret_cast<u32x1*>(qr + (s * TPR + t) * 4) = p[0];
+      else *reinterpret_cast<u32x2*>(qr + (s * TPR + t) * 8) = u32x2{p[0], p[VEC / 4 - 1]};
+    }
+  }
+  if (t < rest) qr[full * VEC + t] = zero ? 0 : (int8_t)q_byte(he * inv);
   if (t == 0) a.out_scale[row] = bad ? __uint_as_float(0x7fc00000u) : (zero ? 0.0f : amax / 127.0f);
 }
+
+template <class DT, class WT, int TPR, int SPT>
+void launch(const NormArgs& a, hipStream_t stream) {
+  const int64_t grid = TPR == 64 ? (a.T + 3) / 4 : a.T;
+  hipLaunchKernelGGL((k_norm<DT, WT, TPR, SPT>), dim3((unsigned)grid), dim3(TPR < 256 ? 256 : TPR), 0, stream, a);
+}
+
+template <class DT, class WT>
+void launch_width(const NormArgs& a, hipStream_t stream) {
+  const int slots = (a.D + DT::VEC - 1) / DT::VEC;
+  if (slots <= 64) launch<DT, WT, 64, 1>(a, stream);
+  else if (slots <= 128) launch<DT, WT, 64, 2>(a, stream);
+  else if (slots <= 256) launch<DT, WT, 256, 1>(a, stream);
+  else if (slots <= 512) launch<DT, WT, 256, 2>(a, stream);
+  else if (slots <= 1024) launch<DT, WT, 256, 4>(a, stream);
+  else if (slots <= 2048) launch<DT, WT, 1024, 2>(a, stream);
+  else if (slots <= 4096) launch<DT, WT, 1024, 4>(a, stream);
+  else if constexpr (DT::VEC == 4) launch<DT, WT, 1024, 8>(a, stream);
+}
+
+static_assert(8 * 1024 * F32T::VEC >= ALBIREO_MAX_NORM_WIDTH && 4 * 1024 * BF16T::VEC >= ALBIREO_MAX_NORM_WIDTH,
+              "the widest row fits");
 
 }  // namespace
 
@@ -115,17 +259,16 @@ albireo_status_t albireo_rms_norm(const void* x, albireo_dtype_t dtype, int64_t 
   a.out = static_cast<unsigned char*>(out);
   a.out_q = out_q;
   a.out_scale = out_scale;
-  a.ldx = ldx, a.ldr = ldr, a.ldro = ldro, a.ldo = ldo, a.ldq = ldq;
+  a.T = T, a.ldx = ldx, a.ldr = ldr, a.ldro = ldro, a.ldo = ldo, a.ldq = ldq;
   a.D = (int32_t)D;
   a.eps = eps;
   const bool wb = weight && weight_dtype == ALBIREO_BF16;
-  const dim3 grid((unsigned)T);
   if (dtype == ALBIREO_BF16) {
-    if (wb) hipLaunchKernelGGL((k_norm<BF16T, BF16T>), grid, dim3(NORM_NT), 0, stream, a);
-    else hipLaunchKernelGGL((k_norm<BF16T, F32T>), grid, dim3(NORM_NT), 0, stream, a);
+    if (wb) launch_width<BF16T, BF16T>(a, stream);
+    else launch_width<BF16T, F32T>(a, stream);
   } else {
-    if (wb) hipLaunchKernelGGL((k_norm<F32T, BF16T>), grid, dim3(NORM_NT), 0, stream, a);
-    else hipLaunchKernelGGL((k_norm<F32T, F32T>), grid, dim3(NORM_NT), 0, stream, a);
+    if (wb) launch_width<F32T, BF16T>(a, stream);
+    else launch_width<F32T, F32T>(a, stream);
   }
   return hipGetLastError() == hipSuccess ? ALBIREO_OK : ALBIREO_E_LAUNCH;
 }
