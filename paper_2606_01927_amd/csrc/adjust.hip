@@ -16,7 +16,9 @@ namespace {
 #include "rows.h"
 
 constexpr int ADJ_NT = 256;
-constexpr int ADJ_TILE = 8192;
+constexpr int ADJ_G = 8;                            // groups of four elements per thread
+constexpr int ADJ_TILE = ADJ_NT * ADJ_G * 4;        // elements per workgroup (32 KB of LDS words)
+constexpr int ADJ_IDS = 8;                          // list entries in flight per thread
 
 struct AdjArgs {
   const unsigned char* logits;
@@ -52,28 +54,107 @@ __device__ __forceinline__ bool csr_range(const int64_t* offsets, int64_t row, i
   return false;
 }
 
-// One tile of one row per workgroup.
-template <class DT, class OT>
+// Four consecutive elements, at an address aligned to the element only (gfx950 takes unaligned vector loads).
+template <class DT>
+struct Four {
+  uint32_t d[DT::ES];
+  __device__ __forceinline__ void load(const unsigned char* p) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(4)));
+    if constexpr (DT::ES == 2) {
+      const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+      d[0] = v.x, d[1] = v.y;
+    } else {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+      d[0] = v.x, d[1] = v.y, d[2] = v.z, d[3] = v.w;
+    }
+  }
+  __device__ __forceinline__ float get(int e) const {
+    if constexpr (DT::ES == 4) return __uint_as_float(d[e]);
+    else return __uint_as_float((e & 1) ? d[e / 2] & 0xffff0000u : d[e / 2] << 16);
+  }
+};
+
+template <class OT>
+__device__ __forceinline__ void store4(unsigned char* p, const float (&v)[4]) {  // p aligned to the four
+  if constexpr (OT::ES == 2) *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+  else *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+}
+
+// f(id, index) for the entries [lo, hi) of a list, ADJ_IDS loads per thread in flight before any is used
+// (an index past the range reloads the first of the group)
+template <class F>
+__device__ __forceinline__ void for_ids(const int32_t* ids, int64_t lo, int64_t hi, F&& f) {
+  for (int64_t h0 = lo + threadIdx.x; h0 < hi; h0 += (int64_t)ADJ_IDS * ADJ_NT) {
+    int32_t v[ADJ_IDS];
+#pragma unroll
+    for (int q = 0; q < ADJ_IDS; ++q) {
+      const int64_t h = h0 + (int64_t)q * ADJ_NT;
+      v[q] = ids[h < hi ? h : h0];
+    }
+#pragma unroll
+    for (int q = 0; q < ADJ_IDS; ++q) {
+      const int64_t h = h0 + (int64_t)q * ADJ_NT;
+      if (h < hi) f(v[q], h);
+    }
+  }
+}
+
+// One tile of one row per workgroup.  Tiles start at the row's first output element whose group of four is
+// aligned (tile 0 also takes the up to three elements before it), so every store but the row's ends is a whole
+// group's whatever V is; loads are as wide, unaligned where the row is.  Each element is read and written by
+// one thread, so the output may be the input.
+//
+// Biases and penalties reach the elements through one 32-bit LDS word each.  First the words take, for every
+// entry of the row's bias list inside the tile, the entry's number (atomic maximum: the last entry of an id
+// wins, whatever the order of the threads), and every element with a word adds that entry's value; then they
+// are cleared and take the histories' counts and prompt marks (the penalty state's encoding).  A row without
+// one of the two skips its half, so a mask alone costs no LDS pass and no barrier.
+//
+// In place, an element is read only where a bias, a penalty or a mask that splits its group of four needs it,
+// and written only where it changes.
+//
+// Bound: HBM.
+template <class DT, class OT, bool IN_PLACE>
 __global__ __launch_bounds__(ADJ_NT) void k_adjust(AdjArgs a) {
-  __shared__ uint32_t word[ADJ_TILE];
-  __shared__ float val[ADJ_TILE];
+  __shared__ __align__(16) uint32_t words[ADJ_TILE + 4];  // word i + 4: element t0 + i
   const int t = threadIdx.x;
   const int64_t row = blockIdx.y;
-  const int64_t t0 = (int64_t)blockIdx.x * ADJ_TILE, t1 = min(a.V, t0 + ADJ_TILE);
-  const unsigned char* xr = a.logits + row * a.ld * DT::ES;
+  const unsigned char* xrow = a.logits + row * a.ld * DT::ES;
   unsigned char* orow = a.out + row * a.ldo * OT::ES;
-  const DevParams& q = a.prm;
+  int head = (int)((-(uint32_t)(reinterpret_cast<uintptr_t>(orow) & (4 * OT::ES - 1)) & (4 * OT::ES - 1)) / OT::ES);
+  if (head > a.V) head = (int)a.V;
+  const int64_t t0 = head + (int64_t)blockIdx.x * ADJ_TILE;  // the tile: [t0, t1), and the head in tile 0
+  const int64_t t1 = min(a.V, t0 + ADJ_TILE);
+  const int ng = t1 > t0 ? (int)((t1 - t0) / 4) : 0;         // whole groups; the rest one by one
+  const int rest = t1 > t0 ? (int)(t1 - t0) - 4 * ng : 0;
+  const bool first = blockIdx.x == 0;
+
+  Four<DT> raw[ADJ_G];
+  if (!IN_PLACE && ng > 0) {  // every load in flight at once (a group past the last reloads the last)
+    static_for<ADJ_G>([&](auto J) {
+      constexpr int j = decltype(J)::value;
+      raw[j].load(xrow + (t0 + 4 * (int64_t)min(j * ADJ_NT + t, ng - 1)) * DT::ES);
+    });
+  }
+  // the elements outside the groups: threads 0-2 the head (tile 0), 4-6 the rest of the last tile
+  int64_t xi = -1;
+  if (first && t < head) xi = t;
+  else if (t >= 4 && t - 4 < rest) xi = t0 + 4 * (int64_t)ng + (t - 4);
+  float xe = xi >= 0 ? DT::load1(xrow, xi) : 0.0f;
+
   uint32_t fl = 0;
+  const DevParams& q = a.prm;
+  int64_t lo, hi, plo, phi, blo, bhi;
+  if (!csr_range(q.hist_offsets, row, q.hist_len, lo, hi)) fl |= FLAG_BAD_PARAM;
+  if (!csr_range(a.prompt_offsets, row, a.prompt_len, plo, phi)) fl |= FLAG_BAD_PARAM;
+  if (!csr_range(a.bias_offsets, row, a.bias_len, blo, bhi)) fl |= FLAG_BAD_PARAM;
   float rep = sload(q.rep ? q.rep + row : &kParamDefaults[3]);
   float freq = sload(q.freq ? q.freq + row : &kParamDefaults[4]);
   float pres = sload(q.pres ? q.pres + row : &kParamDefaults[5]);
   if (!(rep > 0.0f) || isinf(rep)) rep = 1.0f, fl |= FLAG_BAD_PARAM;
   if (!isfinite(freq)) freq = 0.0f, fl |= FLAG_BAD_PARAM;
   if (!isfinite(pres)) pres = 0.0f, fl |= FLAG_BAD_PARAM;
-  int64_t lo, hi, plo, phi, blo, bhi;
-  if (!csr_range(q.hist_offsets, row, q.hist_len, lo, hi)) fl |= FLAG_BAD_PARAM;
-  if (!csr_range(a.prompt_offsets, row, a.prompt_len, plo, phi)) fl |= FLAG_BAD_PARAM;
-  if (!csr_range(a.bias_offsets, row, a.bias_len, blo, bhi)) fl |= FLAG_BAD_PARAM;
   int sn = 0;
   if (a.st_len) {
     sn = sload(a.st_len + row);
@@ -81,57 +162,139 @@ __global__ __launch_bounds__(ADJ_NT) void k_adjust(AdjArgs a) {
   }
   const uint32_t* mrow = nullptr;
   if (a.mask) {
-    int64_t m = row;
-    if (a.mask_index) m = a.mask_index[row];
+    const int64_t m = a.mask_index ? (int64_t)sload(a.mask_index + row) : row;
     if (m >= a.mask_rows) fl |= FLAG_BAD_PARAM;
     else if (m >= 0) mrow = a.mask + m * a.mask_ld;
   }
-  for (int i = t; i < (int)(t1 - t0); i += ADJ_NT) {
-    val[i] = DT::load1(xr, t0 + i);
-    word[i] = 0;
+  // the mask's four bits of each group, set where it lets nothing through
+  const int64_t last_word = (a.V - 1) >> 5;
+  uint32_t gone[ADJ_G];
+  if (mrow && ng > 0) {
+    uint32_t w0[ADJ_G], w1[ADJ_G];
+    static_for<ADJ_G>([&](auto J) {
+      constexpr int j = decltype(J)::value;
+      const int64_t w = (t0 + 4 * (int64_t)min(j * ADJ_NT + t, ng - 1)) >> 5;
+      w0[j] = mrow[w];
+      w1[j] = mrow[min(w + 1, last_word)];
+    });
+    static_for<ADJ_G>([&](auto J) {
+      constexpr int j = decltype(J)::value;
+      const uint32_t sh = (uint32_t)(t0 + 4 * (int64_t)min(j * ADJ_NT + t, ng - 1)) & 31u;
+      gone[j] = ~(uint32_t)((((uint64_t)w1[j] << 32) | w0[j]) >> sh) & 15u;
+    });
+  } else {
+    static_for<ADJ_G>([&](auto J) { gone[decltype(J)::value] = 0u; });
   }
-  __syncthreads();
-  for (int64_t e = blo + t; e < bhi; e += ADJ_NT) {  // the last entry of an id
-    const int32_t id = a.bias_ids[e];
-    if (id < 0 || id >= a.V) fl |= FLAG_BAD_INPUT;
-    else if (isnan(a.bias_values[e])) fl |= FLAG_BAD_PARAM;
-    if (id >= t0 && id < t1) atomicMax(&word[id - t0], (uint32_t)(e - blo) + 1u);
+
+  const int64_t base = t0 - 4;  // element of LDS word 0
+  const int64_t e0 = first ? 0 : t0;
+  uint4* w4 = reinterpret_cast<uint4*>(words);
+  float x[ADJ_G][4];
+  bool have[ADJ_G];  // in place: the group has been read
+  static_for<ADJ_G>([&](auto J) {
+    constexpr int j = decltype(J)::value;
+    have[j] = !IN_PLACE;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[j][e] = IN_PLACE ? 0.0f : raw[j].get(e);
+  });
+  const auto fetch = [&](float (&v)[4], int g) __attribute__((always_inline)) {
+    Four<DT> f;
+    f.load(xrow + (t0 + 4 * (int64_t)g) * DT::ES);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = f.get(e);
+  };
+  bool changed = false;  // of the element xi
+
+  if (bhi > blo) {
+    for (int i = t; i < ADJ_TILE / 4 + 1; i += ADJ_NT) w4[i] = make_uint4(0u, 0u, 0u, 0u);
+    __syncthreads();
+    for_ids(a.bias_ids, blo, bhi, [&](int32_t id, int64_t h) __attribute__((always_inline)) {
+      if (id < 0 || id >= a.V) fl |= FLAG_BAD_INPUT;
+      if (id >= e0 && id < t1) atomicMax(&words[id - base], (uint32_t)(h - blo) + 1u);
+    });
+    if (first && a.flags)
+      for (int64_t h = blo + t; h < bhi; h += ADJ_NT) fl |= isnan(a.bias_values[h]) ? FLAG_BAD_PARAM : 0u;
+    __syncthreads();
+    const float* bv = a.bias_values + blo - 1;
+    const auto add = [&](float& v, uint32_t w) __attribute__((always_inline)) {
+      if (w) {
+        const float b = bv[w];
+        if (!isnan(b)) v = __fadd_rn(v, b);
+      }
+    };
+    static_for<ADJ_G>([&](auto J) {
+      constexpr int j = decltype(J)::value;
+      const int g = j * ADJ_NT + t;
+      if (g < ng) {
+        const uint4 c = w4[g + 1];
+        if (c.x | c.y | c.z | c.w) {
+          if (!have[j]) fetch(x[j], g), have[j] = true;
+          add(x[j][0], c.x);
+          add(x[j][1], c.y);
+          add(x[j][2], c.z);
+          add(x[j][3], c.w);
+        }
+      }
+    });
+    if (xi >= 0 && words[xi - base]) add(xe, words[xi - base]), changed = true;
+    __syncthreads();
   }
-  __syncthreads();
-  for (int i = t; i < (int)(t1 - t0); i += ADJ_NT) {
-    if (word[i]) {
-      const float b = a.bias_values[blo + word[i] - 1];
-      if (!isnan(b)) val[i] = __fadd_rn(val[i], b);
+
+  if (hi > lo || phi > plo || sn > 0) {
+    for (int i = t; i < ADJ_TILE / 4 + 1; i += ADJ_NT) w4[i] = make_uint4(0u, 0u, 0u, 0u);
+    __syncthreads();
+    for_ids(q.hist_ids, lo, hi, [&](int32_t id, int64_t) __attribute__((always_inline)) {
+      if (id < 0 || id >= a.V) fl |= FLAG_BAD_INPUT;
+      if (id >= e0 && id < t1) atomicAdd(&words[id - base], 1u);
+    });
+    for_ids(a.prompt_ids, plo, phi, [&](int32_t id, int64_t) __attribute__((always_inline)) {
+      if (id < 0 || id >= a.V) fl |= FLAG_BAD_INPUT;
+      if (id >= e0 && id < t1) atomicOr(&words[id - base], 0x80000000u);
+    });
+    const uint32_t* sc = a.st_counts + row * a.st_cap;
+    for_ids(a.st_ids + row * a.st_cap, 0, sn, [&](int32_t id, int64_t e) __attribute__((always_inline)) {
+      if (id < 0 || id >= a.V) fl |= FLAG_BAD_INPUT;
+      if (id >= e0 && id < t1) words[id - base] = sc[e];  // distinct ids
+    });
+    __syncthreads();
+    static_for<ADJ_G>([&](auto J) {
+      constexpr int j = decltype(J)::value;
+      const int g = j * ADJ_NT + t;
+      if (g < ng) {
+        const uint4 c = w4[g + 1];
+        if (c.x | c.y | c.z | c.w) {
+          if (!have[j]) fetch(x[j], g), have[j] = true;
+          if (c.x) x[j][0] = penalise_cv(x[j][0], c.x, rep, freq, pres);
+          if (c.y) x[j][1] = penalise_cv(x[j][1], c.y, rep, freq, pres);
+          if (c.z) x[j][2] = penalise_cv(x[j][2], c.z, rep, freq, pres);
+          if (c.w) x[j][3] = penalise_cv(x[j][3], c.w, rep, freq, pres);
+        }
+      }
+    });
+    if (xi >= 0) {
+      const uint32_t c = words[xi - base];
+      if (c) xe = penalise_cv(xe, c, rep, freq, pres), changed = true;
     }
-    word[i] = 0;
   }
-  __syncthreads();
-  for (int64_t e = lo + t; e < hi; e += ADJ_NT) {
-    const int32_t id = q.hist_ids[e];
-    if (id < 0 || id >= a.V) fl |= FLAG_BAD_INPUT;
-    if (id >= t0 && id < t1) atomicAdd(&word[id - t0], 1u);
+
+  static_for<ADJ_G>([&](auto J) {
+    constexpr int j = decltype(J)::value;
+    const int g = j * ADJ_NT + t;
+    if (g < ng) {
+      if (IN_PLACE && !have[j] && gone[j] != 0u && gone[j] != 15u) fetch(x[j], g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (gone[j] >> e & 1u) x[j][e] = -INFINITY;
+      if (!IN_PLACE || have[j] || gone[j]) store4<OT>(orow + (t0 + 4 * (int64_t)g) * OT::ES, x[j]);
+    }
+  });
+  if (xi >= 0) {
+    if (mrow && !(mrow[xi >> 5] >> (xi & 31) & 1u)) xe = -INFINITY, changed = true;
+    if (!IN_PLACE || changed) store1<OT>(orow, xi, xe);
   }
-  for (int64_t e = plo + t; e < phi; e += ADJ_NT) {
-    const int32_t id = a.prompt_ids[e];
-    if (id < 0 || id >= a.V) fl |= FLAG_BAD_INPUT;
-    if (id >= t0 && id < t1) atomicOr(&word[id - t0], 0x80000000u);
-  }
-  for (int e = t; e < sn; e += ADJ_NT) {
-    const int32_t id = a.st_ids[row * a.st_cap + e];
-    if (id < 0 || id >= a.V) fl |= FLAG_BAD_INPUT;
-    if (id >= t0 && id < t1) word[id - t0] = a.st_counts[row * a.st_cap + e];
-  }
-  __syncthreads();
-  for (int i = t; i < (int)(t1 - t0); i += ADJ_NT) {
-    const int64_t v = t0 + i;
-    float x = val[i];
-    if (word[i]) x = penalise_cv(x, word[i], rep, freq, pres);
-    if (mrow && !((mrow[v >> 5] >> (v & 31)) & 1u)) x = -INFINITY;
-    store1<OT>(orow, v, x);
-  }
-  if (a.flags && blockIdx.x == 0) {
-    const uint32_t f1 = __syncthreads_or(fl & FLAG_BAD_INPUT) ? FLAG_BAD_INPUT : 0u;
-    const uint32_t f2 = __syncthreads_or(fl & FLAG_BAD_PARAM) ? FLAG_BAD_PARAM : 0u;
+  if (first && a.flags) {
+    const uint32_t f1 = __syncthreads_or((int)(fl & FLAG_BAD_INPUT)) ? FLAG_BAD_INPUT : 0u;
+    const uint32_t f2 = __syncthreads_or((int)(fl & FLAG_BAD_PARAM)) ? FLAG_BAD_PARAM : 0u;
     if (t == 0) a.flags[row] = f1 | f2 | (a.st_flags ? a.st_flags[row] : 0u);
   }
 }
@@ -198,12 +361,15 @@ albireo_status_t albireo_adjust_logits(const void* logits, albireo_dtype_t dtype
     a.mask_index = constraints->mask_index;
   }
   const dim3 grid((unsigned)((V + ADJ_TILE - 1) / ADJ_TILE), (unsigned)B), nt(ADJ_NT);
+  const bool in_place = out == logits, ob = out_dtype == ALBIREO_BF16;
   if (dtype == ALBIREO_BF16) {
-    if (out_dtype == ALBIREO_BF16) hipLaunchKernelGGL((k_adjust<BF16T, BF16T>), grid, nt, 0, stream, a);
-    else hipLaunchKernelGGL((k_adjust<BF16T, F32T>), grid, nt, 0, stream, a);
+    if (in_place) hipLaunchKernelGGL((k_adjust<BF16T, BF16T, true>), grid, nt, 0, stream, a);
+    else if (ob) hipLaunchKernelGGL((k_adjust<BF16T, BF16T, false>), grid, nt, 0, stream, a);
+    else hipLaunchKernelGGL((k_adjust<BF16T, F32T, false>), grid, nt, 0, stream, a);
   } else {
-    if (out_dtype == ALBIREO_BF16) hipLaunchKernelGGL((k_adjust<F32T, BF16T>), grid, nt, 0, stream, a);
-    else hipLaunchKernelGGL((k_adjust<F32T, F32T>), grid, nt, 0, stream, a);
+    if (in_place) hipLaunchKernelGGL((k_adjust<F32T, F32T, true>), grid, nt, 0, stream, a);
+    else if (ob) hipLaunchKernelGGL((k_adjust<F32T, BF16T, false>), grid, nt, 0, stream, a);
+    else hipLaunchKernelGGL((k_adjust<F32T, F32T, false>), grid, nt, 0, stream, a);
   }
   return hipGetLastError() == hipSuccess ? ALBIREO_OK : ALBIREO_E_LAUNCH;
 }
