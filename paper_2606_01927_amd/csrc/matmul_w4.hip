@@ -21,7 +21,9 @@ struct W4Args {
   unsigned char* out;
   int64_t ldx, ldq, lds, ldz, ldo;
   int64_t N;
-  int32_t B, K, n_blocks, m_blocks;
+  int32_t B, K;
+  int32_t n_blocks, m_blocks;          // k_w4: weight and row blocks
+  int32_t wg_tiles, wg_more;           // k_w4_stream: weight tiles of a workgroup, workgroups with one more
   bool scale_bf16, out_bf16;
 };
 
@@ -48,24 +50,15 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(1)));
+typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(1)));  // gfx950 takes unaligned vector loads
+typedef uint32_t u32x2a2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4a4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32a1 __attribute__((aligned(1)));
 
+#ifndef SB
+#define SB 3
+#endif
 constexpr int W4_NT = 256;  // threads per workgroup
-
-template <int CTRL>
-__device__ __forceinline__ uint32_t dpp_full(uint32_t v) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
-}
-
-// Sum over aligned groups of L = 2, 4, 8 or 16 lanes (every lane receives it).
-template <int L, class Add>
-__device__ __forceinline__ uint32_t group_sum(uint32_t v, Add add) {
-  v = add(v, dpp_full<0xb1>(v));                      // quad_perm 1,0,3,2
-  if constexpr (L >= 4) v = add(v, dpp_full<0x4e>(v));   // quad_perm 2,3,0,1
-  if constexpr (L >= 8) v = add(v, dpp_full<0x141>(v));  // row_half_mirror
-  if constexpr (L >= 16) v = add(v, dpp_full<0x140>(v)); // row_mirror
-  return v;
-}
 
 // a's upper 32 lanes against b's lower 32
 __device__ __forceinline__ void swap32(uint32_t& a, uint32_t& b) {
@@ -78,6 +71,169 @@ __device__ __forceinline__ void swap16(uint32_t& a, uint32_t& b) {
   const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
   a = r[0];
   b = r[1];
+}
+
+// 16 bytes of a row with the columns of every eight in the order the nibbles of a dword come out
+template <bool I8>
+__device__ __forceinline__ u32x4 nibble_order(const u32x4 v) {
+  u32x4 p;
+  if constexpr (I8) {  // columns 0 2 4 6 | 1 3 5 7
+    p[0] = __builtin_amdgcn_perm(v[1], v[0], 0x06040200u);
+    p[1] = __builtin_amdgcn_perm(v[1], v[0], 0x07050301u);
+    p[2] = __builtin_amdgcn_perm(v[3], v[2], 0x06040200u);
+    p[3] = __builtin_amdgcn_perm(v[3], v[2], 0x07050301u);
+  } else {  // columns 0 2 | 4 6 | 1 3 | 5 7
+    p[0] = __builtin_amdgcn_perm(v[1], v[0], 0x05040100u);
+    p[1] = __builtin_amdgcn_perm(v[3], v[2], 0x05040100u);
+    p[2] = __builtin_amdgcn_perm(v[1], v[0], 0x07060302u);
+    p[3] = __builtin_amdgcn_perm(v[3], v[2], 0x07060302u);
+  }
+  return p;
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_full(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+
+// The sum of the values of an aligned group of L = 2, 4, 8 or 16 lanes, 16 bytes each (every lane receives it).
+template <bool I8, int L>
+__device__ __forceinline__ float group_sum(const u32x4 v) {
+  uint32_t s;
+  if constexpr (I8) {
+    int n = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) n = __builtin_amdgcn_sdot4((int)v[e], 0x01010101, n, false);
+    s = (uint32_t)n;
+  } else {
+    float f = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f += __uint_as_float(v[e] << 16) + __uint_as_float(v[e] & 0xffff0000u);
+    s = __float_as_uint(f);
+  }
+  const auto add = [](uint32_t x, uint32_t y) __attribute__((always_inline)) {
+    return I8 ? x + y : __float_as_uint(__uint_as_float(x) + __uint_as_float(y));
+  };
+  s = add(s, dpp_full<0xb1>(s));                         // quad_perm 1 0 3 2
+  if constexpr (L >= 4) s = add(s, dpp_full<0x4e>(s));   // quad_perm 2 3 0 1
+  if constexpr (L >= 8) s = add(s, dpp_full<0x141>(s));  // row_half_mirror
+  if constexpr (L >= 16) s = add(s, dpp_full<0x140>(s)); // row_mirror
+  return I8 ? (float)(int)s : __uint_as_float(s);
+}
+
+// The A operands of 128 columns of a lane's row (p: the row's first of them in LDS), in the order by_group leaves
+// the weights in.
+template <bool I8, int G>
+__device__ __forceinline__ void load_rows(u32x4 (&xa)[I8 ? 2 : 4], const unsigned char* p, int q4) {
+#pragma unroll
+  for (int i = 0; i < (I8 ? 2 : 4); ++i) {
+    if constexpr (!I8) {  // eight columns
+      int k;
+      if constexpr (G == 128) k = q4 * 32 + i * 8;
+      else if constexpr (G == 64) k = (i >> 1) * 64 + (q4 & 1) * 32 + (i & 1) * 16 + (q4 >> 1) * 8;
+      else k = i * 32 + q4 * 8;
+      xa[i] = *reinterpret_cast<const u32x4*>(p + k * 2);
+    } else if constexpr (G == 128) {  // sixteen columns
+      xa[i] = *reinterpret_cast<const u32x4*>(p + q4 * 32 + i * 16);
+    } else if constexpr (G == 64) {
+      xa[i] = *reinterpret_cast<const u32x4*>(p + i * 64 + (q4 & 1) * 32 + (q4 >> 1) * 16);
+    } else {  // eight columns of two groups of 32
+      const uint2 lo = *reinterpret_cast<const uint2*>(p + (2 * i) * 32 + q4 * 8);
+      const uint2 hi = *reinterpret_cast<const uint2*>(p + (2 * i + 1) * 32 + q4 * 8);
+      xa[i] = u32x4{lo.x, lo.y, hi.x, hi.y};
+    }
+  }
+}
+
+// The four dwords a lane loads are 32 columns, so with groups of 64 or 32 the lanes of one load hold different
+// groups: swaps between lanes put each group's columns into the same registers (two, or one).
+template <bool I8, int G>
+__device__ __forceinline__ void by_group(uint32_t (&d)[4]) {
+  if constexpr (G == 64 && !I8) {
+    swap32(d[0], d[1]);  // d0: group 0 (columns 0-7 and 8-15 of the two lanes), d1: group 1
+    swap32(d[2], d[3]);
+    const uint32_t e = d[1];
+    d[1] = d[2];
+    d[2] = e;
+  } else if constexpr (G == 64) {
+    swap32(d[0], d[2]);
+    swap32(d[1], d[3]);
+  } else if constexpr (G == 32) {
+    swap32(d[0], d[2]);
+    swap32(d[1], d[3]);
+    swap16(d[0], d[1]);
+    swap16(d[2], d[3]);
+  }
+}
+
+// Where the sums of group g of 128 columns start: -8 sum x, x against a constant on the matrix units.
+template <bool I8, int G>
+__device__ __forceinline__ u32x4 group_start(const u32x4 (&xa)[I8 ? 2 : 4], int g) {
+  constexpr int GS = 128 / G;
+  if constexpr (!I8) {
+    const u32x4 cv = {0xc100c100u, 0xc100c100u, 0xc100c100u, 0xc100c100u};
+    f32x4 r = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = g * (4 / GS); i < (g + 1) * (4 / GS); ++i)
+      r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xa[i]), __builtin_bit_cast(bf16x8, cv), r, 0, 0, 0);
+    return __builtin_bit_cast(u32x4, r);
+  } else {
+    i32x4 r = {0, 0, 0, 0};
+    if constexpr (G == 32) {
+      const u32x4 x4 = xa[g >> 1];
+      const uint64_t xv = (g & 1) ? ((uint64_t)x4[3] << 32 | x4[2]) : ((uint64_t)x4[1] << 32 | x4[0]);
+      r = __builtin_amdgcn_mfma_i32_16x16x32_i8((long)xv, (long)0xf8f8f8f8f8f8f8f8ull, r, 0, 0, 0);
+    } else {
+      const i32x4 cv = {(int)0xf8f8f8f8u, (int)0xf8f8f8f8u, (int)0xf8f8f8f8u, (int)0xf8f8f8f8u};
+#pragma unroll
+      for (int i = g * (2 / GS); i < (g + 1) * (2 / GS); ++i)
+        r = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, xa[i]), cv, r, 0, 0, 0);
+    }
+    return __builtin_bit_cast(u32x4, r);
+  }
+}
+
+// two bytes of four as bf16: q
+__device__ __forceinline__ uint32_t pair_of(uint32_t b, bool high) {
+  return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 512.0f, true))
+              : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 512.0f, false));
+}
+
+// r[m] += the columns of group g of rows m times their weights' q.
+template <bool I8, int G, int MT>
+__device__ __forceinline__ void multiply_group(u32x4 (&r)[MT], const u32x4 (&xa)[MT][I8 ? 2 : 4], const uint32_t (&d)[4], int g) {
+  constexpr int GS = 128 / G;
+  if constexpr (!I8) {
+#pragma unroll
+    for (int i = g * (4 / GS); i < (g + 1) * (4 / GS); ++i) {
+      // a byte 0x0q is the 8-bit float (4 exponent bits, 3 of mantissa) q 2^-9, denormal or not
+      const uint32_t lo = d[i] & 0x0f0f0f0fu, hi = (d[i] >> 4) & 0x0f0f0f0fu;
+      const u32x4 wv = {pair_of(lo, false), pair_of(lo, true), pair_of(hi, false), pair_of(hi, true)};
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+        r[m] = __builtin_bit_cast(u32x4, __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            __builtin_bit_cast(bf16x8, xa[m][i]), __builtin_bit_cast(bf16x8, wv), __builtin_bit_cast(f32x4, r[m]), 0, 0, 0));
+    }
+  } else if constexpr (G == 32) {
+    const uint64_t wv = (uint64_t)((d[g] >> 4) & 0x0f0f0f0fu) << 32 | (d[g] & 0x0f0f0f0fu);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const u32x4 x4 = xa[m][g >> 1];
+      const uint64_t xv = (g & 1) ? ((uint64_t)x4[3] << 32 | x4[2]) : ((uint64_t)x4[1] << 32 | x4[0]);
+      r[m] = __builtin_bit_cast(u32x4, __builtin_amdgcn_mfma_i32_16x16x32_i8((long)xv, (long)wv,
+                                                                            __builtin_bit_cast(i32x4, r[m]), 0, 0, 0));
+    }
+  } else {
+#pragma unroll
+    for (int i = g * (2 / GS); i < (g + 1) * (2 / GS); ++i) {
+      const u32x4 wv = {d[2 * i] & 0x0f0f0f0fu, (d[2 * i] >> 4) & 0x0f0f0f0fu, d[2 * i + 1] & 0x0f0f0f0fu,
+                        (d[2 * i + 1] >> 4) & 0x0f0f0f0fu};
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+        r[m] = __builtin_bit_cast(u32x4, __builtin_amdgcn_mfma_i32_16x16x64_i8(
+            __builtin_bit_cast(i32x4, xa[m][i]), __builtin_bit_cast(i32x4, wv), __builtin_bit_cast(i32x4, r[m]), 0, 0, 0));
+    }
+  }
 }
 
 template <bool I8, int G, int MT, int NT, int WK, int KC>
@@ -94,14 +250,13 @@ struct W4Shape {
   static_assert(XU % W4_NT == 0, "whole units per thread");
   struct Buf {
     alignas(16) unsigned char x[ROWS * XST];
-    alignas(16) float sum[NG][ROWS];               // sum of x over a group (8 bits: its integer's value)
     alignas(16) float scale[NG][RN];
-    alignas(16) float off[NG][RN];                 // scale (8 - zero)
+    alignas(16) float off[NG][RN];                 // with zero points: scale (zero - 8) / 8, against -8 sum x
   };
 };
 
-template <bool I8, int G, int MT, int NT, int WK, int KC>
-__global__ __launch_bounds__(W4_NT) void k_w4(W4Args a) {
+template <bool I8, int G, class ST, bool Z, int MT, int NT, int WK, int KC, int PD, int MW>
+__global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
   using S = W4Shape<I8, G, MT, NT, WK, KC>;
   __shared__ typename S::Buf buf[2];
   const int t = threadIdx.x, lane = lane_id(), wave = wave_id();
@@ -133,80 +288,48 @@ __global__ __launch_bounds__(W4_NT) void k_w4(W4Args a) {
 #pragma unroll
   for (int j = 0; j < NT; ++j) wrow[j] = a.q + (n0 + min(wn + j * 16 + c16, rn - 1)) * a.ldq;
 
-  // staging: unit i of this thread is 16 bytes of one row; a group of columns lies in GL adjacent lanes
+  // staging: unit i of this thread is 16 bytes of one row
   constexpr int UPR = KC * S::ES / 16;          // units per row
-  constexpr int GL = G * S::ES / 16;
-  u32x4 xr[S::XPT];
-  float sr[S::SPT];
-  int zr[S::SPT];
-  auto load_x = [&](int k0) __attribute__((always_inline)) {
+  struct Stage {  // what the next chunks need in LDS, on its way
+    u32x4 x[S::XPT];
+    uint32_t s[S::SPT];
+    uint8_t z[S::SPT];
+  };
+  // rows past the last repeat it (and are not staged); columns past K repeat the row's end, under scales of zero
+  const unsigned char* xbase = a.x + (int64_t)b0 * a.ldx * S::ES;
+  uint32_t xoff[S::XPT];
+#pragma unroll
+  for (int i = 0; i < S::XPT; ++i) xoff[i] = (uint32_t)min((t + i * W4_NT) / UPR, rows - 1) * (uint32_t)a.ldx;
+  auto load_x = [&](Stage& st, int k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < S::XPT; ++i) {
-      const int u = t + i * W4_NT, r = u / UPR, k = k0 + (u % UPR) * (16 / S::ES);
-      xr[i] = u32x4{0, 0, 0, 0};
-      if (r < rows && k < a.K)
-        xr[i] = *reinterpret_cast<const u32x4u*>(a.x + ((int64_t)(b0 + r) * a.ldx + k) * S::ES);
+      const int k = min(k0 + (t + i * W4_NT) % UPR * (16 / S::ES), a.K - 16 / S::ES);
+      st.x[i] = *reinterpret_cast<const u32x4u*>(xbase + (xoff[i] + (uint32_t)k) * S::ES);
     }
-  };
-  auto load_s = [&](int k0) __attribute__((always_inline)) {
     const int g0 = k0 / G;
 #pragma unroll
     for (int i = 0; i < S::SPT; ++i) {
-      const int u = t + i * W4_NT, r = u / S::NG, g = g0 + u % S::NG;
-      sr[i] = 0.0f;
-      zr[i] = 8;
-      if (r < rn && g < groups) {
-        const int64_t at = (n0 + r) * a.lds + g;
-        sr[i] = a.scale_bf16 ? BF16T::load1(a.scales, at) : F32T::load1(a.scales, at);
-        if (a.zeros) zr[i] = a.zeros[(n0 + r) * a.ldz + g];
-      }
+      const int u = t + i * W4_NT;
+      const int64_t r = n0 + min(u / S::NG, rn - 1);
+      const int g = min(g0 + u % S::NG, groups - 1);
+      if constexpr (ST::ES == 2) st.s[i] = reinterpret_cast<const uint16_t*>(a.scales)[r * a.lds + g];
+      else st.s[i] = reinterpret_cast<const uint32_t*>(a.scales)[r * a.lds + g];
+      if constexpr (Z) st.z[i] = a.zeros[r * a.ldz + g];
     }
   };
-  auto put = [&](typename S::Buf& b) __attribute__((always_inline)) {
+  auto put = [&](const Stage& st, typename S::Buf& b, int k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < S::XPT; ++i) {
       const int u = t + i * W4_NT, r = u / UPR, c = u % UPR;
-      const u32x4 v = xr[i];
-      u32x4 p;
-      float sum;
-      if constexpr (I8) {
-        int s = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_sdot4((int)v[e], 0x01010101, s, false);
-        s = (int)group_sum<GL>((uint32_t)s, [](uint32_t x, uint32_t y) { return x + y; });
-        sum = (float)s;
-        // columns 0 2 4 6 | 1 3 5 7 of each eight
-        p[0] = __builtin_amdgcn_perm(v[1], v[0], 0x06040200u);
-        p[1] = __builtin_amdgcn_perm(v[1], v[0], 0x07050301u);
-        p[2] = __builtin_amdgcn_perm(v[3], v[2], 0x06040200u);
-        p[3] = __builtin_amdgcn_perm(v[3], v[2], 0x07050301u);
-      } else {
-        float s = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s += __uint_as_float(v[e] << 16);
-          s += __uint_as_float(v[e] & 0xffff0000u);
-        }
-        sum = __uint_as_float(group_sum<GL>(__float_as_uint(s), [](uint32_t x, uint32_t y) {
-          return __float_as_uint(__uint_as_float(x) + __uint_as_float(y));
-        }));
-        // columns 0 4 | 1 5 | 2 6 | 3 7
-        p[0] = __builtin_amdgcn_perm(v[2], v[0], 0x05040100u);
-        p[1] = __builtin_amdgcn_perm(v[2], v[0], 0x07060302u);
-        p[2] = __builtin_amdgcn_perm(v[3], v[1], 0x05040100u);
-        p[3] = __builtin_amdgcn_perm(v[3], v[1], 0x07060302u);
-      }
-      if (r < rows) {
-        *reinterpret_cast<u32x4*>(b.x + r * S::XST + c * 16) = p;
-        if ((lane & (GL - 1)) == 0) b.sum[c / GL][r] = sum;
-      }
+      if (r < rows) *reinterpret_cast<u32x4*>(b.x + r * S::XST + c * 16) = nibble_order<I8>(st.x[i]);
     }
 #pragma unroll
     for (int i = 0; i < S::SPT; ++i) {
       const int u = t + i * W4_NT, r = u / S::NG, g = u % S::NG;
       if (S::RN * S::NG % W4_NT == 0 || r < S::RN) {
-        b.scale[g][r] = I8 ? sr[i] : 16.0f * sr[i];
-        if (a.zeros) b.off[g][r] = sr[i] * (float)(8 - zr[i]);
+        const float sc = k0 / G + g < groups ? __uint_as_float(ST::ES == 2 ? st.s[i] << 16 : st.s[i]) : 0.0f;
+        b.scale[g][r] = sc;
+        if constexpr (Z) b.off[g][r] = sc * (0.125f * (float)((int)st.z[i] - 8));
       }
     }
   };
@@ -225,145 +348,81 @@ __global__ __launch_bounds__(W4_NT) void k_w4(W4Args a) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) total[m][j] = f32x4{0, 0, 0, 0};
 
-  // Columns of step s (128) of the chunk: the operands of its instructions are NI sets; set i lies in group
-  // i CH / ... of the step.  Where a group is 64 or 32 columns, the lanes of a load hold different groups, and
-  // swaps between them put each group's columns into the same registers.
-  constexpr int NI = I8 ? (G == 32 ? 4 : 2) : 4;  // instructions per 128 columns
   constexpr int GS = 128 / G;                     // groups per 128 columns
   auto multiply = [&](u32x4 (&w)[NT][S::KS], typename S::Buf& b, int k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < S::KS; ++s) {
       const int ks = s * WK + wk;  // the step in the chunk
       if (k0 + ks * 128 >= a.K) break;
-      u32x4 xa[MT][4];  // the step's columns of x, in the order of the weights below
+      u32x4 xa[MT][I8 ? 2 : 4];
+      uint32_t d[NT][4];
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const unsigned char* xrow = b.x + (m * 16 + c16) * S::XST + ks * 128 * S::ES;
-#pragma unroll
-        for (int i = 0; i < (I8 ? 2 : 4); ++i) {
-          int k;  // first of the 8 (bf16) or 16 (8 bits) columns
-          if constexpr (!I8) {
-            if constexpr (G == 128) k = q4 * 32 + i * 8;
-            else if constexpr (G == 64) k = (i >> 1) * 64 + (q4 & 1) * 32 + (i & 1) * 16 + (q4 >> 1) * 8;
-            else k = i * 32 + q4 * 8;
-            xa[m][i] = *reinterpret_cast<const u32x4*>(xrow + k * 2);
-          } else if constexpr (G == 128) {
-            xa[m][i] = *reinterpret_cast<const u32x4*>(xrow + q4 * 32 + i * 16);
-          } else if constexpr (G == 64) {
-            xa[m][i] = *reinterpret_cast<const u32x4*>(xrow + i * 64 + (q4 & 1) * 32 + (q4 >> 1) * 16);
-          } else {  // two groups of 32: eight columns of each
-            const uint2 lo = *reinterpret_cast<const uint2*>(xrow + (2 * i) * 32 + q4 * 8);
-            const uint2 hi = *reinterpret_cast<const uint2*>(xrow + (2 * i + 1) * 32 + q4 * 8);
-            xa[m][i] = u32x4{lo.x, lo.y, hi.x, hi.y};
-          }
-        }
-      }
-      f32x4 sums[MT][GS];
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int g = 0; g < GS; ++g)
-          sums[m][g] = *reinterpret_cast<const f32x4*>(&b.sum[ks * GS + g][m * 16 + q4 * 4]);
+      for (int m = 0; m < MT; ++m) load_rows<I8, G>(xa[m], b.x + (m * 16 + c16) * S::XST + ks * 128 * S::ES, q4);
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        uint32_t d0 = w[j][s][0], d1 = w[j][s][1], d2 = w[j][s][2], d3 = w[j][s][3];
-        if constexpr (G == 64 && !I8) {
-          swap32(d0, d1);  // d0: group 0 (columns 0-7 and 8-15 of the two lanes), d1: group 1
-          swap32(d2, d3);
-          const uint32_t e = d1;
-          d1 = d2;  // d0, d1: group 0; d2, d3: group 1
-          d2 = e;
-        } else if constexpr (G == 64) {
-          swap32(d0, d2);  // (d0, d1): group 0, (d2, d3): group 1
-          swap32(d1, d3);
-        } else if constexpr (G == 32) {  // d[i]: group i
-          swap32(d0, d2);
-          swap32(d1, d3);
-          swap16(d0, d1);
-          swap16(d2, d3);
-        }
-        const uint32_t d[4] = {d0, d1, d2, d3};
-        u32x4 wb[NI];
-        if constexpr (!I8) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            wb[i][0] = ((d[i] << 3) & 0x00780078u) | 0x3f803f80u;
-            wb[i][1] = ((d[i] >> 1) & 0x00780078u) | 0x3f803f80u;
-            wb[i][2] = ((d[i] >> 5) & 0x00780078u) | 0x3f803f80u;
-            wb[i][3] = ((d[i] >> 9) & 0x00780078u) | 0x3f803f80u;
-          }
-        } else if constexpr (G != 32) {
+        for (int e = 0; e < 4; ++e) d[j][e] = w[j][s][e];
+        by_group<I8, G>(d[j]);
+      }
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
-            wb[i] = u32x4{d[2 * i] & 0x0f0f0f0fu, (d[2 * i] >> 4) & 0x0f0f0f0fu, d[2 * i + 1] & 0x0f0f0f0fu,
-                          (d[2 * i + 1] >> 4) & 0x0f0f0f0fu};
-        }
+      for (int g = 0; g < GS; ++g) {
+        u32x4 start[MT];
+        float scale[NT];
 #pragma unroll
-        for (int g = 0; g < GS; ++g) {
-          const float sc = b.scale[ks * GS + g][wn + j * 16 + c16];
+        for (int m = 0; m < MT; ++m) start[m] = group_start<I8, G>(xa[m], g);
 #pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            f32x4 r;
-            if constexpr (I8) {
-              i32x4 c;
+        for (int j = 0; j < NT; ++j) scale[j] = b.scale[ks * GS + g][wn + j * 16 + c16];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) c[e] = (int)(-8.0f * sums[m][g][e]);
-              if constexpr (G == 32) {
-                const u32x4 x4 = xa[m][g >> 1];
-                const uint64_t xx = (g & 1) ? ((uint64_t)x4[3] << 32 | x4[2]) : ((uint64_t)x4[1] << 32 | x4[0]);
-                const uint64_t ww = (uint64_t)((d[g] >> 4) & 0x0f0f0f0fu) << 32 | (d[g] & 0x0f0f0f0fu);
-                c = __builtin_amdgcn_mfma_i32_16x16x32_i8((long)xx, (long)ww, c, 0, 0, 0);
-              } else {
+        for (int j = 0; j < NT; ++j) {
+          u32x4 r[MT];
 #pragma unroll
-                for (int i = 0; i < 2 / GS; ++i)
-                  c = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, xa[m][g * (2 / GS) + i]),
-                                                            __builtin_bit_cast(i32x4, wb[g * (2 / GS) + i]), c, 0, 0, 0);
-              }
+          for (int m = 0; m < MT; ++m) r[m] = start[m];
+          multiply_group<I8, G, MT>(r, xa, d[j], g);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) r[e] = (float)c[e];
-            } else {
+          for (int m = 0; m < MT; ++m)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) r[e] = -1.5f * sums[m][g][e];
-#pragma unroll
-              for (int i = 0; i < 4 / GS; ++i)
-                r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xa[m][g * (4 / GS) + i]),
-                                                            __builtin_bit_cast(bf16x8, wb[g * (4 / GS) + i]), r, 0, 0, 0);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) total[m][j][e] = fmaf(r[e], sc, total[m][j][e]);
-          }
-          if (a.zeros) {
-            const float of = b.off[ks * GS + g][wn + j * 16 + c16];
+            for (int e = 0; e < 4; ++e)
+              total[m][j][e] = fmaf(I8 ? (float)(int)r[m][e] : __uint_as_float(r[m][e]), scale[j], total[m][j][e]);
+          if constexpr (Z) {
+            const float off = b.off[ks * GS + g][wn + j * 16 + c16];
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) total[m][j][e] = fmaf(sums[m][g][e], of, total[m][j][e]);
+              for (int e = 0; e < 4; ++e)
+                total[m][j][e] = fmaf(I8 ? (float)(int)start[m][e] : __uint_as_float(start[m][e]), off, total[m][j][e]);
           }
+          // no further: the next weights unpacked ahead of their products would not fit the registers
+          if constexpr (SB & 1) __builtin_amdgcn_sched_barrier(0);
         }
       }
+      if constexpr (SB & 2) __builtin_amdgcn_sched_barrier(0);
     }
   };
 
-  u32x4 wa[NT][S::KS], wb[NT][S::KS];
-  load_x(0);
-  load_s(0);
-  load_w(wa, 0);
-  put(buf[0]);
-  // one chunk: the next one's loads go out, this one is multiplied, the next one's x goes to LDS
-  auto chunk = [&](int k0, u32x4 (&cur)[NT][S::KS], u32x4 (&nxt)[NT][S::KS], int at) __attribute__((always_inline)) {
-    const bool more = k0 + KC < a.K;
-    if (more) {
-      load_x(k0 + KC);
-      load_s(k0 + KC);
-      load_w(nxt, k0 + KC);
-    }
-    __syncthreads();
-    multiply(cur, buf[at], k0);
-    if (more) put(buf[at ^ 1]);
-  };
-  for (int k0 = 0; k0 < a.K; k0 += 2 * KC) {
-    chunk(k0, wa, wb, 0);
-    if (k0 + KC < a.K) chunk(k0 + KC, wb, wa, 1);
+  // PD chunks are on their way: x and scales of chunk c + PD go out as chunk c starts, its weights as chunk c's
+  // have been used, and the staging of chunk c + 1 is written to LDS at the end of chunk c.
+  u32x4 wr[PD][NT][S::KS];
+  Stage st[PD];
+  static_for<PD>([&](auto I) {
+    constexpr int i = decltype(I)::value;
+    load_x(st[i], i * KC);
+    load_w(wr[i], i * KC);
+  });
+  put(st[0], buf[0], 0);
+  int at = 0;
+  // Without a branch: a chunk past K loads row ends and counts as zeros, so the registers on their way are waited
+  // for at their use alone.
+  for (int k1 = 0; k1 < a.K; k1 += PD * KC) {
+    static_for<PD>([&](auto I) {
+      constexpr int i = decltype(I)::value;
+      const int k0 = k1 + i * KC;
+      __syncthreads();
+      load_x(st[i], k0 + PD * KC);
+      multiply(wr[i], buf[at], k0);
+      load_w(wr[i], k0 + PD * KC);
+      at ^= 1;
+      put(st[(i + 1) % PD], buf[at], k0 + KC);
+    });
   }
 
   if constexpr (WK > 1) {  // join the waves' shares: wave 0 adds the others' in order
@@ -407,27 +466,314 @@ __global__ __launch_bounds__(W4_NT) void k_w4(W4Args a) {
   }
 }
 
-template <bool I8, int G, int MT, int NT, int WK, int KC>
+// ----------------------------------------------------------------------------------------------
+// Few rows.
+//
+// When the rows of x fit a CU's LDS whole (in the order of the nibbles, zeros behind the last column up to whole
+// quads of groups), one workgroup of sixteen waves per CU stages them once and then streams weights without a
+// barrier: the workgroup has a contiguous range of 16-row weight tiles, its waves equal shares of the range's
+// quads of groups, whatever tile they begin in, and each keeps R quads of loads on their way.  The tiles that two
+// or more waves share are joined through LDS at the end, by the wave that holds the tile's first columns, in the
+// order of the waves.
+// ----------------------------------------------------------------------------------------------
+constexpr int W4S_NT = 1024;
+constexpr int W4S_WAVES = W4S_NT / 64;
+constexpr int W4S_LDS = 160 * 1024;
+constexpr int W4S_WGS = 256;
+#ifndef W4_FEW
+#define W4_FEW 8
+#define W4_RA (G == 128 ? 1 : G == 64 ? 2 : 3)
+#define W4_RB (G == 128 ? 2 : G == 64 ? 2 : 3)
+#endif
+
+template <bool I8, int G, int MT>
+struct W4StreamShape {
+  static constexpr int ES = I8 ? 1 : 2;
+  static constexpr int QC = 4 * G;        // columns of a quad of groups
+  static constexpr int KQ = QC / 128;     // 128-column steps of a quad
+  static constexpr int ROWS = MT * 16;
+  // LDS: the rows, and their sum over each group
+  static int64_t quads(int64_t K) { return (K + QC - 1) / QC; }
+  static constexpr int XU = 8;            // 16-byte units of a row of x a lane asks for at once
+  static int64_t bytes(int64_t B, int64_t K) { return B * (K * ES + 16) + K / G * ROWS * 4; }
+};
+
+template <bool I8, int G, class ST, bool Z, int MT, int R>
+__global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
+  using S = W4StreamShape<I8, G, MT>;
+  constexpr int ES = S::ES, KQ = S::KQ, GS = 128 / G;
+  __shared__ __align__(16) unsigned char lds[W4S_LDS];
+  const int t = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
+  const int c16 = lane & 15, q4 = lane >> 4;
+  const int rows = a.B, groups = a.K / G;
+  const int nq = (groups + 3) / 4;
+  const int upr = a.K * ES / 16, xst = a.K * ES + 16;
+  float* xsum = reinterpret_cast<float*>(lds + rows * xst);  // [groups][ROWS]
+
+  // Staging: a wave takes a row of x at a time.  The first of it is asked for ahead of the weights, by every wave
+  // before any wave asks for weights: loads return in order, and all of x is needed before the first product.
+  u32x4 xv[S::XU];
+  const auto load_x = [&](int r, int first) __attribute__((always_inline)) {
+    const unsigned char* p = a.x + (int64_t)r * a.ldx * ES;
+#pragma unroll
+    for (int i = 0; i < S::XU; ++i) xv[i] = *reinterpret_cast<const u32x4u*>(p + min(first + i * 64 + lane, upr - 1) * 16);
+  };
+  const auto put_x = [&](int r, int first) __attribute__((always_inline)) {
+    constexpr int L = G * ES / 16;  // a group of columns lies in L neighbouring lanes
+    unsigned char* p = lds + r * xst;
+    float* sp = xsum + r;
+#pragma unroll
+    for (int i = 0; i < S::XU; ++i) {
+      const int u = first + i * 64 + lane;
+      if (u < upr) {
+        *reinterpret_cast<u32x4*>(p + u * 16) = nibble_order<I8>(xv[i]);
+        const float sum = group_sum<I8, L>(xv[i]);
+        if (lane % L == 0) sp[u / L * S::ROWS] = sum;
+      }
+    }
+  };
+  if (wave < rows) load_x(wave, 0);
+  __builtin_amdgcn_s_barrier();
+
+  // the workgroup's tiles and the wave's share [qa, qb) of their quads
+  const int ntiles = a.wg_tiles + (blockIdx.x < (uint32_t)a.wg_more);
+  const uint32_t t0 = blockIdx.x * a.wg_tiles + min((int)blockIdx.x, a.wg_more);
+  const uint32_t nquads = (uint32_t)ntiles * nq;
+  const uint32_t qa = nquads * wave / W4S_WAVES, qb = nquads * (wave + 1) / W4S_WAVES;
+  const uint32_t ta = qa / (uint32_t)nq;
+
+  struct Quad {
+    u32x4 w[KQ];
+    uint32_t s[ST::ES == 2 ? 2 : 4];
+    uint32_t z;
+  };
+  Quad ring[R];
+  // The next quad to ask for.  The last tile is the last 16 rows whatever N is (and stores those past the tile
+  // before), so a lane's distance from its tile's first row never changes; past the share's end the asking goes on
+  // into the next wave's quads, and past the last tile it stays there.
+  uint32_t pt = t0 + ta;
+  int pk = (int)(qa - ta * nq);
+  const uint32_t wlane = c16 * (uint32_t)a.ldq + q4 * 16, slane = c16 * (uint32_t)a.lds * ST::ES, zlane = c16 * (uint32_t)a.ldz;
+  int64_t prow = min((int64_t)pt * 16, a.N - 16);
+  const uint8_t* wtile = a.q + prow * a.ldq;
+  const unsigned char* stile = a.scales + prow * a.lds * ST::ES;
+  const uint8_t* ztile = Z ? a.zeros + prow * a.ldz : nullptr;
+  auto ask = [&](Quad& d) __attribute__((always_inline)) {
+    // The last quad of a row is its last four groups: what it has of the quad before counts with a scale of 0.
+    const int g = min(pk * 4, groups - 4);
+    const uint8_t* wr = wtile + g * (G / 2);
+#pragma unroll
+    for (int s = 0; s < KQ; ++s) d.w[s] = *reinterpret_cast<const u32x4u*>(wr + wlane + s * 64);
+    const unsigned char* sr = stile + g * ST::ES;
+    if constexpr (ST::ES == 2) {
+      const u32x2a2 v = *reinterpret_cast<const u32x2a2*>(sr + slane);
+      d.s[0] = v.x, d.s[1] = v.y;
+    } else {
+      const u32x4a4 v = *reinterpret_cast<const u32x4a4*>(sr + slane);
+      d.s[0] = v.x, d.s[1] = v.y, d.s[2] = v.z, d.s[3] = v.w;
+    }
+    if constexpr (Z) d.z = *reinterpret_cast<const u32a1*>(ztile + g + zlane);
+    if (++pk == nq) {
+      pk = 0;
+      prow = min((int64_t)++pt * 16, a.N - 16);
+      wtile = a.q + prow * a.ldq;
+      stile = a.scales + prow * a.lds * ST::ES;
+      if constexpr (Z) ztile = a.zeros + prow * a.ldz;
+    }
+  };
+  static_for<R>([&](auto I) { ask(ring[decltype(I)::value]); });
+
+  if (wave < rows) put_x(wave, 0);
+  for (int r = wave; r < rows; r += W4S_WAVES)
+    for (int u = r == wave ? S::XU * 64 : 0; u < upr; u += S::XU * 64) {
+      load_x(r, u);
+      put_x(r, u);
+    }
+  __syncthreads();
+
+  const unsigned char* xrow[MT];  // rows past the last repeat it
+#pragma unroll
+  for (int m = 0; m < MT; ++m) xrow[m] = lds + min(m * 16 + c16, rows - 1) * xst;
+  f32x4 total[MT], head[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) total[m] = head[m] = f32x4{0, 0, 0, 0};
+  uint32_t ct = t0 + ta;
+  int ck = (int)(qa - ta * nq);
+  bool whole = ck == 0;  // the tile at hand began in this share
+  const auto store = [&](const f32x4 (&v)[MT], uint32_t tile) __attribute__((always_inline)) {
+    const int64_t n = min((int64_t)tile * 16, a.N - 16) + c16;
+    if (n < (int64_t)tile * 16) return;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const int b = m * 16 + q4 * 4, left = rows - b;
+      f32x4 r = v[m];
+      if constexpr (I8) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] *= a.x_scale[min(b + e, rows - 1)];
+      }
+      if (a.out_bf16) {
+        uint16_t* o = reinterpret_cast<uint16_t*>(a.out) + b * a.ldo + n;
+#pragma unroll
+        for (int e = 0; e < 4; ++e, o += a.ldo)
+          if (e < left) *o = (uint16_t)bf16_pair(r[e], r[e]);
+      } else {
+        float* o = reinterpret_cast<float*>(a.out) + b * a.ldo + n;
+#pragma unroll
+        for (int e = 0; e < 4; ++e, o += a.ldo)
+          if (e < left) *o = r[e];
+      }
+    }
+  };
+  for (uint32_t q = qa; q < qb; q += R) {
+    f32x4 done[MT];  // a tile finished in these R quads (a tile has at least as many)
+    bool finished = false;
+    static_for<R>([&](auto I) {
+      constexpr int i = decltype(I)::value;
+      if (q + i < qb) {
+        Quad& d = ring[i];
+        const int g0 = min(ck * 4, groups - 4), again = ck * 4 - g0;  // first group, and how many the quad before had
+        float sc[4];
+        if constexpr (ST::ES == 2) {
+          uint64_t s = (uint64_t)d.s[1] << 32 | d.s[0];
+          if (again) s &= ~(uint64_t)0 << (16 * again);
+          sc[0] = __uint_as_float((uint32_t)s << 16);
+          sc[1] = __uint_as_float((uint32_t)s & 0xffff0000u);
+          sc[2] = __uint_as_float((uint32_t)(s >> 32) << 16);
+          sc[3] = __uint_as_float((uint32_t)(s >> 32) & 0xffff0000u);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[e] = e < again ? 0.0f : __uint_as_float(d.s[e]);
+        }
+        // the zero points' share of the four groups: one fp32 instruction, lane q4 * 16 + c16 giving group q4
+        const float s01 = (q4 & 1) ? sc[1] : sc[0], s23 = (q4 & 1) ? sc[3] : sc[2];
+        const float off = ((q4 & 2) ? s23 : s01) * (Z ? -(float)(d.z >> (8 * q4) & 0xffu) : -8.0f);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+          total[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(xsum[(g0 + q4) * S::ROWS + m * 16 + c16], off, total[m], 0, 0, 0);
+#pragma unroll
+        for (int s = 0; s < KQ; ++s) {
+          u32x4 xa[MT][I8 ? 2 : 4];
+#pragma unroll
+          for (int m = 0; m < MT; ++m) load_rows<I8, G>(xa[m], xrow[m] + (g0 * G + s * 128) * ES, q4);
+          uint32_t dw[4] = {d.w[s][0], d.w[s][1], d.w[s][2], d.w[s][3]};
+          by_group<I8, G>(dw);
+#pragma unroll
+          for (int g = 0; g < GS; ++g) {
+            u32x4 r[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) r[m] = u32x4{0, 0, 0, 0};
+            multiply_group<I8, G, MT>(r, xa, dw, g);
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                total[m][e] = fmaf(I8 ? (float)(int)r[m][e] : __uint_as_float(r[m][e]), sc[s * GS + g], total[m][e]);
+          }
+        }
+        if (++ck == nq) {
+          if (whole) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) done[m] = total[m];
+          } else {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) head[m] = total[m];
+          }
+          finished = whole;
+#pragma unroll
+          for (int m = 0; m < MT; ++m) total[m] = f32x4{0, 0, 0, 0};
+          ck = 0, ++ct;
+          whole = true;
+        }
+      }
+      ask(ring[i]);
+    });
+    if (finished) store(done, ct - 1);
+  }
+
+  // join the shared tiles: what a wave holds of a tile begun before its share goes through LDS
+  __syncthreads();
+  f32x4* part = reinterpret_cast<f32x4*>(lds);
+  const bool inner = !whole;  // the share ends in the tile it began inside
+#pragma unroll
+  for (int m = 0; m < MT; ++m) part[(wave * MT + m) * 64 + lane] = inner ? total[m] : head[m];
+  __syncthreads();
+  if (qb > qa && whole && ck != 0) {
+    const uint32_t end = (ct - t0 + 1) * nq;  // the tile's end among the workgroup's quads
+    for (int w = wave + 1; w < W4S_WAVES; ++w) {
+      const uint32_t wa = nquads * w / W4S_WAVES, wb = nquads * (w + 1) / W4S_WAVES;
+      if (wa >= end) break;
+      if (wb > wa) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) total[m] += part[(w * MT + m) * 64 + lane];
+      }
+    }
+    store(total, ct);
+  }
+}
+
+template <bool I8, int G, int MT, int NT, int WK, int KC, int PD, int MW>
 hipError_t launch(W4Args& a, hipStream_t stream) {
   using S = W4Shape<I8, G, MT, NT, WK, KC>;
   const int64_t nb = (a.N + S::RN - 1) / S::RN, mb = (a.B + S::ROWS - 1) / S::ROWS;
   if (nb * mb >= ((int64_t)1 << 31)) return hipErrorInvalidConfiguration;
   a.n_blocks = (int32_t)nb;
   a.m_blocks = (int32_t)mb;
-  hipLaunchKernelGGL((k_w4<I8, G, MT, NT, WK, KC>), dim3((unsigned)(nb * mb)), dim3(W4_NT), 0, stream, a);
+  const dim3 grid((unsigned)(nb * mb)), nt(W4_NT);
+  if (a.scale_bf16) {
+    if (a.zeros) hipLaunchKernelGGL((k_w4<I8, G, BF16T, true, MT, NT, WK, KC, PD, MW>), grid, nt, 0, stream, a);
+    else hipLaunchKernelGGL((k_w4<I8, G, BF16T, false, MT, NT, WK, KC, PD, MW>), grid, nt, 0, stream, a);
+  } else {
+    if (a.zeros) hipLaunchKernelGGL((k_w4<I8, G, F32T, true, MT, NT, WK, KC, PD, MW>), grid, nt, 0, stream, a);
+    else hipLaunchKernelGGL((k_w4<I8, G, F32T, false, MT, NT, WK, KC, PD, MW>), grid, nt, 0, stream, a);
+  }
   return hipGetLastError();
 }
 
-// Tiles by the number of rows: as many 16-row operands as the rows fill, up to four, so that a weight is
-// unpacked once for up to 64 rows.
+template <bool I8, int G, int MT, int R>
+hipError_t launch_stream(W4Args& a, hipStream_t stream) {
+  const int64_t tiles = (a.N + 15) / 16, wgs = tiles < W4S_WGS ? tiles : W4S_WGS;
+  a.wg_tiles = (int32_t)(tiles / wgs);
+  a.wg_more = (int32_t)(tiles % wgs);
+  const dim3 grid((unsigned)wgs), nt(W4S_NT);
+  if (a.scale_bf16) {
+    if (a.zeros) hipLaunchKernelGGL((k_w4_stream<I8, G, BF16T, true, MT, R>), grid, nt, 0, stream, a);
+    else hipLaunchKernelGGL((k_w4_stream<I8, G, BF16T, false, MT, R>), grid, nt, 0, stream, a);
+  } else {
+    if (a.zeros) hipLaunchKernelGGL((k_w4_stream<I8, G, F32T, true, MT, R>), grid, nt, 0, stream, a);
+    else hipLaunchKernelGGL((k_w4_stream<I8, G, F32T, false, MT, R>), grid, nt, 0, stream, a);
+  }
+  return hipGetLastError();
+}
+
+// Whether k_w4_stream<I8, G, MT> takes the shape: a whole tile and whole quads of groups, the rows in LDS, shares
+// and a tile's strides in 32 bits.
+template <bool I8, int G, int MT>
+bool streams(const W4Args& a) {
+  using S = W4StreamShape<I8, G, MT>;
+  return a.B <= S::ROWS && a.N >= 16 && S::quads(a.K) >= 3 && a.K >= S::QC && S::bytes(a.B, a.K) <= W4S_LDS &&
+         ((a.N + 15) / 16 / W4S_WGS + 1) * S::quads(a.K) < ((int64_t)1 << 27) && a.ldq < ((int64_t)1 << 27) &&
+         a.lds < ((int64_t)1 << 24) && a.ldz < ((int64_t)1 << 27);
+}
+
+template <bool I8, int G, int MT>
+hipError_t stream_rows(W4Args& a, hipStream_t stream) {
+  constexpr int QUADS = W4_FEW;
+  const int64_t share = (a.N + 15) / 16 * W4StreamShape<I8, G, MT>::quads(a.K) / (W4S_WGS * W4S_WAVES);
+  if (share < QUADS) return launch_stream<I8, G, MT, W4_RA>(a, stream);
+  return launch_stream<I8, G, MT, W4_RB>(a, stream);
+}
+
 template <bool I8, int G>
 hipError_t launch_rows(W4Args& a, hipStream_t stream) {
+  if (streams<I8, G, 1>(a)) return stream_rows<I8, G, 1>(a, stream);
+  if (streams<I8, G, 2>(a)) return stream_rows<I8, G, 2>(a, stream);
   if (a.B <= 16) {
-    if (a.N < 16384) return launch<I8, G, 1, 1, 4, 1024>(a, stream);
-    return launch<I8, G, 1, 2, 1, 512>(a, stream);
+    if (a.N < 16384) return launch<I8, G, 1, 1, 4, 512, 2, 3>(a, stream);
+    return launch<I8, G, 1, 2, 1, 256, 2, 3>(a, stream);
   }
-  if (a.B <= 32) return launch<I8, G, 2, 2, 1, 256>(a, stream);
-  return launch<I8, G, 4, 4, 1, 128>(a, stream);
+  if (a.B <= 32) return launch<I8, G, 2, 2, 1, 256, 1, 2>(a, stream);
+  constexpr int NT = I8 && G == 128 ? 4 : 2, KC = !I8 && G < 128 ? 128 : 256;
+  return launch<I8, G, 4, NT, 1, KC, 1, 2>(a, stream);
 }
 
 }  // namespace
@@ -447,7 +793,7 @@ albireo_status_t albireo_matmul_w4(const void* x, albireo_rows_t x_type, int64_t
   if (w.ldq < w.K / 2 || w.lds < w.K / w.group || (w.zeros && w.ldz < w.K / w.group)) return ALBIREO_E_INVALID;
   const bool i8 = x_type == ALBIREO_ROWS_I8;
   if (!i8 && x_scale) return ALBIREO_E_INVALID;
-  if (B > 65535 || w.N >= ((int64_t)1 << 31) - 1024 || w.K >= ((int64_t)1 << 24)) return ALBIREO_E_UNSUPPORTED;
+  if (B > 65535 || ldx >= ((int64_t)1 << 24) || w.N >= ((int64_t)1 << 31) - 1024 || w.K >= ((int64_t)1 << 24)) return ALBIREO_E_UNSUPPORTED;
   const auto off = [](const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; };
   if (off(x, i8 ? 1 : 2) || off(x_scale, 4) || off(out, out_dtype == ALBIREO_BF16 ? 2 : 4) ||
       off(w.scales, w.scale_dtype == ALBIREO_BF16 ? 2 : 4))
