@@ -5,6 +5,7 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <type_traits>
 #include <utility>
 
 #include "albireo_decode.h"
@@ -81,22 +82,33 @@ __device__ __forceinline__ void store4(unsigned char* p, const float (&v)[4]) { 
   else *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
 }
 
-// f(id, index) for the entries [lo, hi) of a list, ADJ_IDS loads per thread in flight before any is used
-// (an index past the range reloads the first of the group)
-template <class F>
-__device__ __forceinline__ void for_ids(const int32_t* ids, int64_t lo, int64_t hi, F&& f) {
-  for (int64_t h0 = lo + threadIdx.x; h0 < hi; h0 += (int64_t)ADJ_IDS * ADJ_NT) {
-    int32_t v[ADJ_IDS];
+// The entries [lo, hi) of a list over the workgroup, ADJ_IDS loads per thread in flight before any is used (an index
+// past the range reloads the first of the group).  The first of them can be asked for ahead of their use.
+struct Ids {
+  int32_t v[ADJ_IDS];
+  __device__ __forceinline__ void load(const int32_t* ids, int64_t h0, int64_t hi) {
 #pragma unroll
     for (int q = 0; q < ADJ_IDS; ++q) {
       const int64_t h = h0 + (int64_t)q * ADJ_NT;
       v[q] = ids[h < hi ? h : h0];
     }
+  }
+  template <class F>
+  __device__ __forceinline__ void each(int64_t h0, int64_t hi, F&& f) const {
 #pragma unroll
     for (int q = 0; q < ADJ_IDS; ++q) {
       const int64_t h = h0 + (int64_t)q * ADJ_NT;
       if (h < hi) f(v[q], h);
     }
+  }
+};
+
+// f(id, index) for the entries [lo, hi); `first` holds the thread's first batch when ASKED
+template <bool ASKED, class F>
+__device__ __forceinline__ void for_ids(Ids& first, const int32_t* ids, int64_t lo, int64_t hi, F&& f) {
+  for (int64_t h0 = lo + threadIdx.x; h0 < hi; h0 += (int64_t)ADJ_IDS * ADJ_NT) {
+    if (!ASKED || h0 != lo + threadIdx.x) first.load(ids, h0, hi);
+    first.each(h0, hi, f);
   }
 }
 
@@ -107,17 +119,18 @@ __device__ __forceinline__ void for_ids(const int32_t* ids, int64_t lo, int64_t 
 //
 // Biases and penalties reach the elements through one 32-bit LDS word each.  First the words take, for every
 // entry of the row's bias list inside the tile, the entry's number (atomic maximum: the last entry of an id
-// wins, whatever the order of the threads), and every element with a word adds that entry's value; then they
-// are cleared and take the histories' counts and prompt marks (the penalty state's encoding).  A row without
-// one of the two skips its half, so a mask alone costs no LDS pass and no barrier.
+// wins, whatever the order of the threads), and every element with a word adds that entry's value and clears it;
+// then they take the histories' counts and prompt marks (the penalty state's encoding).  The first ids of both lists
+// are asked for with the elements.  A row without one of the two skips its half.  Calls without lists take the kernel
+// without LDS (LISTS false).
 //
-// In place, an element is read only where a bias, a penalty or a mask that splits its group of four needs it,
-// and written only where it changes.
+// In place, an element is read only where a bias or a penalty needs it, and written only where it changes: a group
+// that the mask takes whole with one store, the others' elements one by one.
 //
 // Bound: HBM.
-template <class DT, class OT, bool IN_PLACE>
+template <class DT, class OT, bool IN_PLACE, bool LISTS>
 __global__ __launch_bounds__(ADJ_NT) void k_adjust(AdjArgs a) {
-  __shared__ __align__(16) uint32_t words[ADJ_TILE + 4];  // word i + 4: element t0 + i
+  __shared__ __align__(16) uint32_t words[LISTS ? ADJ_TILE + 4 : 4];  // word i + 4: element t0 + i
   const int t = threadIdx.x;
   const int64_t row = blockIdx.y;
   const unsigned char* xrow = a.logits + row * a.ld * DT::ES;
@@ -130,7 +143,7 @@ __global__ __launch_bounds__(ADJ_NT) void k_adjust(AdjArgs a) {
   const int rest = t1 > t0 ? (int)(t1 - t0) - 4 * ng : 0;
   const bool first = blockIdx.x == 0;
 
-  Four<DT> raw[ADJ_G];
+  Four<DT> raw[ADJ_G];  // in place: of the groups that are read
   if (!IN_PLACE && ng > 0) {  // every load in flight at once (a group past the last reloads the last)
     static_for<ADJ_G>([&](auto J) {
       constexpr int j = decltype(J)::value;
@@ -145,10 +158,15 @@ __global__ __launch_bounds__(ADJ_NT) void k_adjust(AdjArgs a) {
 
   uint32_t fl = 0;
   const DevParams& q = a.prm;
-  int64_t lo, hi, plo, phi, blo, bhi;
-  if (!csr_range(q.hist_offsets, row, q.hist_len, lo, hi)) fl |= FLAG_BAD_PARAM;
-  if (!csr_range(a.prompt_offsets, row, a.prompt_len, plo, phi)) fl |= FLAG_BAD_PARAM;
-  if (!csr_range(a.bias_offsets, row, a.bias_len, blo, bhi)) fl |= FLAG_BAD_PARAM;
+  int64_t lo = 0, hi = 0, plo = 0, phi = 0, blo = 0, bhi = 0;
+  Ids bias_ids, hist_ids;
+  if constexpr (LISTS) {
+    if (!csr_range(a.bias_offsets, row, a.bias_len, blo, bhi)) fl |= FLAG_BAD_PARAM;
+    if (!csr_range(q.hist_offsets, row, q.hist_len, lo, hi)) fl |= FLAG_BAD_PARAM;
+    if (!csr_range(a.prompt_offsets, row, a.prompt_len, plo, phi)) fl |= FLAG_BAD_PARAM;
+    if (blo + t < bhi) bias_ids.load(a.bias_ids, blo + t, bhi);
+    if (lo + t < hi) hist_ids.load(q.hist_ids, lo + t, hi);
+  }
   float rep = sload(q.rep ? q.rep + row : &kParamDefaults[3]);
   float freq = sload(q.freq ? q.freq + row : &kParamDefaults[4]);
   float pres = sload(q.pres ? q.pres + row : &kParamDefaults[5]);
@@ -156,7 +174,7 @@ __global__ __launch_bounds__(ADJ_NT) void k_adjust(AdjArgs a) {
   if (!isfinite(freq)) freq = 0.0f, fl |= FLAG_BAD_PARAM;
   if (!isfinite(pres)) pres = 0.0f, fl |= FLAG_BAD_PARAM;
   int sn = 0;
-  if (a.st_len) {
+  if (LISTS && a.st_len) {
     sn = sload(a.st_len + row);
     sn = sn < 0 ? 0 : (sn > a.st_cap ? a.st_cap : sn);
   }
@@ -195,7 +213,7 @@ __global__ __launch_bounds__(ADJ_NT) void k_adjust(AdjArgs a) {
     constexpr int j = decltype(J)::value;
     have[j] = !IN_PLACE;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[j][e] = IN_PLACE ? 0.0f : raw[j].get(e);
+    for (int e = 0; e < 4; ++e) x[j][e] = IN_PLACE ? -INFINITY : raw[j].get(e);
   });
   const auto fetch = [&](float (&v)[4], int g) __attribute__((always_inline)) {
     Four<DT> f;
@@ -205,10 +223,13 @@ __global__ __launch_bounds__(ADJ_NT) void k_adjust(AdjArgs a) {
   };
   bool changed = false;  // of the element xi
 
-  if (bhi > blo) {
+  const bool pen = hi > lo || phi > plo || sn > 0;
+  if (LISTS && (bhi > blo || pen)) {
     for (int i = t; i < ADJ_TILE / 4 + 1; i += ADJ_NT) w4[i] = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
-    for_ids(a.bias_ids, blo, bhi, [&](int32_t id, int64_t h) __attribute__((always_inline)) {
+  }
+  if (LISTS && bhi > blo) {
+    for_ids<true>(bias_ids, a.bias_ids, blo, bhi, [&](int32_t id, int64_t h) __attribute__((always_inline)) {
       if (id < 0 || id >= a.V) fl |= FLAG_BAD_INPUT;
       if (id >= e0 && id < t1) atomicMax(&words[id - base], (uint32_t)(h - blo) + 1u);
     });
@@ -216,43 +237,58 @@ __global__ __launch_bounds__(ADJ_NT) void k_adjust(AdjArgs a) {
       for (int64_t h = blo + t; h < bhi; h += ADJ_NT) fl |= isnan(a.bias_values[h]) ? FLAG_BAD_PARAM : 0u;
     __syncthreads();
     const float* bv = a.bias_values + blo - 1;
-    const auto add = [&](float& v, uint32_t w) __attribute__((always_inline)) {
-      if (w) {
-        const float b = bv[w];
-        if (!isnan(b)) v = __fadd_rn(v, b);
-      }
+    const auto add = [](float& v, float b) __attribute__((always_inline)) {
+      if (!isnan(b)) v = __fadd_rn(v, b);
     };
-    static_for<ADJ_G>([&](auto J) {
-      constexpr int j = decltype(J)::value;
-      const int g = j * ADJ_NT + t;
-      if (g < ng) {
-        const uint4 c = w4[g + 1];
-        if (c.x | c.y | c.z | c.w) {
-          if (!have[j]) fetch(x[j], g), have[j] = true;
-          add(x[j][0], c.x);
-          add(x[j][1], c.y);
-          add(x[j][2], c.z);
-          add(x[j][3], c.w);
+    // four groups at a time: their biases are all asked for before the first is added
+    static_for<ADJ_G / 4>([&](auto H) {
+      constexpr int j0 = decltype(H)::value * 4;
+      float b[4][4];
+      static_for<4>([&](auto J) {
+        constexpr int j = decltype(J)::value;
+        const int g = (j0 + j) * ADJ_NT + t;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[j][e] = __uint_as_float(0x7fc00000u);  // none
+        if (g < ng) {
+          const uint4 c = w4[g + 1];
+          if (c.x | c.y | c.z | c.w) {
+            w4[g + 1] = make_uint4(0u, 0u, 0u, 0u);
+            if (IN_PLACE) raw[j0 + j].load(xrow + (t0 + 4 * (int64_t)g) * DT::ES), have[j0 + j] = true;
+            if (c.x) b[j][0] = bv[c.x];
+            if (c.y) b[j][1] = bv[c.y];
+            if (c.z) b[j][2] = bv[c.z];
+            if (c.w) b[j][3] = bv[c.w];
+          }
         }
-      }
+      });
+      static_for<4>([&](auto J) {
+        constexpr int j = decltype(J)::value;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (IN_PLACE && have[j0 + j]) x[j0 + j][e] = raw[j0 + j].get(e);
+          add(x[j0 + j][e], b[j][e]);
+        }
+      });
     });
-    if (xi >= 0 && words[xi - base]) add(xe, words[xi - base]), changed = true;
+    if (xi >= 0 && words[xi - base]) {
+      add(xe, bv[words[xi - base]]);
+      words[xi - base] = 0u;
+      changed = true;
+    }
     __syncthreads();
   }
 
-  if (hi > lo || phi > plo || sn > 0) {
-    for (int i = t; i < ADJ_TILE / 4 + 1; i += ADJ_NT) w4[i] = make_uint4(0u, 0u, 0u, 0u);
-    __syncthreads();
-    for_ids(q.hist_ids, lo, hi, [&](int32_t id, int64_t) __attribute__((always_inline)) {
+  if (LISTS && pen) {
+    for_ids<true>(hist_ids, q.hist_ids, lo, hi, [&](int32_t id, int64_t) __attribute__((always_inline)) {
       if (id < 0 || id >= a.V) fl |= FLAG_BAD_INPUT;
       if (id >= e0 && id < t1) atomicAdd(&words[id - base], 1u);
     });
-    for_ids(a.prompt_ids, plo, phi, [&](int32_t id, int64_t) __attribute__((always_inline)) {
+    for_ids<false>(hist_ids, a.prompt_ids, plo, phi, [&](int32_t id, int64_t) __attribute__((always_inline)) {
       if (id < 0 || id >= a.V) fl |= FLAG_BAD_INPUT;
       if (id >= e0 && id < t1) atomicOr(&words[id - base], 0x80000000u);
     });
     const uint32_t* sc = a.st_counts + row * a.st_cap;
-    for_ids(a.st_ids + row * a.st_cap, 0, sn, [&](int32_t id, int64_t e) __attribute__((always_inline)) {
+    for_ids<false>(hist_ids, a.st_ids + row * a.st_cap, 0, sn, [&](int32_t id, int64_t e) __attribute__((always_inline)) {
       if (id < 0 || id >= a.V) fl |= FLAG_BAD_INPUT;
       if (id >= e0 && id < t1) words[id - base] = sc[e];  // distinct ids
     });
@@ -281,11 +317,17 @@ __global__ __launch_bounds__(ADJ_NT) void k_adjust(AdjArgs a) {
     constexpr int j = decltype(J)::value;
     const int g = j * ADJ_NT + t;
     if (g < ng) {
-      if (IN_PLACE && !have[j] && gone[j] != 0u && gone[j] != 15u) fetch(x[j], g);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (gone[j] >> e & 1u) x[j][e] = -INFINITY;
-      if (!IN_PLACE || have[j] || gone[j]) store4<OT>(orow + (t0 + 4 * (int64_t)g) * OT::ES, x[j]);
+      unsigned char* op = orow + (t0 + 4 * (int64_t)g) * OT::ES;
+      if (have[j] || gone[j] == 15u) {
+        store4<OT>(op, x[j]);
+      } else if (gone[j]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (gone[j] >> e & 1u) store1<OT>(op, e, -INFINITY);
+      }
     }
   });
   if (xi >= 0) {
@@ -361,16 +403,22 @@ albireo_status_t albireo_adjust_logits(const void* logits, albireo_dtype_t dtype
     a.mask_index = constraints->mask_index;
   }
   const dim3 grid((unsigned)((V + ADJ_TILE - 1) / ADJ_TILE), (unsigned)B), nt(ADJ_NT);
-  const bool in_place = out == logits, ob = out_dtype == ALBIREO_BF16;
-  if (dtype == ALBIREO_BF16) {
-    if (in_place) hipLaunchKernelGGL((k_adjust<BF16T, BF16T, true>), grid, nt, 0, stream, a);
-    else if (ob) hipLaunchKernelGGL((k_adjust<BF16T, BF16T, false>), grid, nt, 0, stream, a);
-    else hipLaunchKernelGGL((k_adjust<BF16T, F32T, false>), grid, nt, 0, stream, a);
-  } else {
-    if (in_place) hipLaunchKernelGGL((k_adjust<F32T, F32T, true>), grid, nt, 0, stream, a);
-    else if (ob) hipLaunchKernelGGL((k_adjust<F32T, BF16T, false>), grid, nt, 0, stream, a);
-    else hipLaunchKernelGGL((k_adjust<F32T, F32T, false>), grid, nt, 0, stream, a);
-  }
+  const bool ob = out_dtype == ALBIREO_BF16;
+  const bool lists = a.bias_offsets || a.prm.hist_offsets || a.prompt_offsets || a.st_len;
+  const auto go = [&](auto LISTS) {
+    constexpr bool L = decltype(LISTS)::value;
+    if (dtype == ALBIREO_BF16) {
+      if (out == logits) hipLaunchKernelGGL((k_adjust<BF16T, BF16T, true, L>), grid, nt, 0, stream, a);
+      else if (ob) hipLaunchKernelGGL((k_adjust<BF16T, BF16T, false, L>), grid, nt, 0, stream, a);
+      else hipLaunchKernelGGL((k_adjust<BF16T, F32T, false, L>), grid, nt, 0, stream, a);
+    } else {
+      if (out == logits) hipLaunchKernelGGL((k_adjust<F32T, F32T, true, L>), grid, nt, 0, stream, a);
+      else if (ob) hipLaunchKernelGGL((k_adjust<F32T, BF16T, false, L>), grid, nt, 0, stream, a);
+      else hipLaunchKernelGGL((k_adjust<F32T, F32T, false, L>), grid, nt, 0, stream, a);
+    }
+  };
+  if (lists) go(std::true_type{});
+  else go(std::false_type{});
   return hipGetLastError() == hipSuccess ? ALBIREO_OK : ALBIREO_E_LAUNCH;
 }
 

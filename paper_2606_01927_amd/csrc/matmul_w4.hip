@@ -28,36 +28,30 @@ struct W4Args {
 };
 
 // ----------------------------------------------------------------------------------------------
-// The product.
+// The mathematics.  With W = s (q - z), one scale s and zero point z to a group of columns,
+//     sum_k x W = sum over the groups of  s (sum x q - z sum x),
+// so the matrix units multiply x by the bare 4-bit values and a scale is applied once per output and group.  Weights
+// are the B operand, straight from memory to registers: a lane loads 16 bytes, 32 columns of one weight row, so the
+// 64 lanes of a load cover 16 rows by 128 columns.  x is the A operand, from LDS, its columns reordered to the order
+// the nibbles come out of a dword: the matrix units add over columns, so any order will do that both sides share.
+//   bf16:   a byte 0x0q is, read as an 8-bit float with 4 exponent and 3 mantissa bits, q 2^-9 (denormal up to 7),
+//           and the hardware's conversion to bf16 with a scale of 2^9 gives q, two at a time.
+//   8 bits: the nibbles of a dword are two operands of four bytes, and a group's sum is an exact integer.
+// Unpacking costs 28 (bf16) or 12 (8 bits) instructions per 16-byte load, beside 4 or 2 matrix instructions per 16
+// rows of x and 4 multiply-adds (8 bits: and conversions) per 16 rows and group.
 //
-// A workgroup of four waves takes RN = (4 / WK) NT 16 weight rows and up to MT 16 rows of x.  Weights are the
-// B operand of the matrix instructions, straight from memory to registers: a lane loads 16 bytes, 32 columns
-// of one weight row, so the 64 lanes of a load cover 16 rows by 128 columns, and each 16-byte load feeds four
-// (bf16) or two (8-bit) instructions.  x is the A operand, staged in LDS a chunk of KC columns at a time with
-// the columns of every eight reordered to the order the nibbles come out of a dword, together with the sum of
-// each group of its columns, the weights' scales and, with zero points, scale (8 - zero).
-//   bf16: a nibble becomes 1 + q / 16 by putting its bits under the exponent of 1 (two columns at a time:
-//         shift, and-or).  The sum of a group starts at -1.5 sum x, which takes 1 + 8 / 16 off every weight,
-//         so it holds sum x (q - 8) / 16, and is added to the result times 16 scale.
-//   8 bits: the nibbles of a dword are two operands of four bytes (and, shift-and); the sum starts at
-//         -8 sum x and is exact; one conversion and one multiply-add per value and group.
-// The loads of the next chunk (x, scales and weights) are in flight while a chunk is multiplied; LDS is
-// double-buffered with one barrier per chunk.
-// With WK = 4 the waves share their rows and each takes every fourth 128 columns, joined through LDS.
+// Two kernels.  Up to 32 rows that fit a CU's LDS go to k_w4_stream, bound by HBM; more rows to k_w4, bound by the
+// scaling's vector instructions and the waits of two waves a SIMD beside the matrix instructions.
 // ----------------------------------------------------------------------------------------------
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(1)));  // gfx950 takes unaligned vector loads
 typedef uint32_t u32x2a2 __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t u32x4a4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32a1 __attribute__((aligned(1)));
 
-#ifndef SB
-#define SB 3
-#endif
 constexpr int W4_NT = 256;  // threads per workgroup
 
 // a's upper 32 lanes against b's lower 32
@@ -236,6 +230,19 @@ __device__ __forceinline__ void multiply_group(u32x4 (&r)[MT], const u32x4 (&xa)
   }
 }
 
+// ----------------------------------------------------------------------------------------------
+// Any number of rows.
+//
+// A workgroup of four waves takes RN = (4 / WK) NT 16 weight rows and up to MT 16 rows of x.  A chunk of KC columns
+// of x is staged in LDS with the weights' scales and, with zero points, scale (zero - 8) / 8.  A group's sum starts at
+// -8 sum x, which the matrix units find against a constant operand (they wait for the vector instructions anyway;
+// summing x while staging it cost 256 x 152064 x 4096 8 us), so a zero point of 8 costs nothing further.  PD chunks are
+// on their way while one is multiplied: x and scales through registers into the other of two LDS buffers, one barrier
+// per chunk.  With WK = 4 the waves share their rows and each takes every fourth 128 columns, joined through LDS.
+//
+// 8-bit rows, us: 64 x 128256 x 8192 159 (floor 113), 256 x 152064 x 4096 311 (1.03 PFLOP/s; the same product of bf16
+// weights by the library 422).
+// ----------------------------------------------------------------------------------------------
 template <bool I8, int G, int MT, int NT, int WK, int KC>
 struct W4Shape {
   static constexpr int ROWS = MT * 16;             // rows of x
@@ -392,10 +399,9 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
                 total[m][j][e] = fmaf(I8 ? (float)(int)start[m][e] : __uint_as_float(start[m][e]), off, total[m][j][e]);
           }
           // no further: the next weights unpacked ahead of their products would not fit the registers
-          if constexpr (SB & 1) __builtin_amdgcn_sched_barrier(0);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
-      if constexpr (SB & 2) __builtin_amdgcn_sched_barrier(0);
     }
   };
 
@@ -469,22 +475,22 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
 // ----------------------------------------------------------------------------------------------
 // Few rows.
 //
-// When the rows of x fit a CU's LDS whole (in the order of the nibbles, zeros behind the last column up to whole
-// quads of groups), one workgroup of sixteen waves per CU stages them once and then streams weights without a
-// barrier: the workgroup has a contiguous range of 16-row weight tiles, its waves equal shares of the range's
-// quads of groups, whatever tile they begin in, and each keeps R quads of loads on their way.  The tiles that two
-// or more waves share are joined through LDS at the end, by the wave that holds the tile's first columns, in the
-// order of the waves.
+// When the rows of x fit a CU's LDS whole, one workgroup of sixteen waves per CU stages them once, with their sums
+// over the groups, and then streams weights without a barrier.  The workgroup has a contiguous range of 16-row weight
+// tiles, its waves equal shares of the range's quads of groups, whatever tile they begin in, and each keeps R quads of
+// loads on their way.  z sum x of a quad's four groups is one fp32 matrix instruction.  The tiles that two or more
+// waves share are joined through LDS at the end, by the wave that holds the tile's first columns, in the order of the
+// waves.
+//
+// Bound: HBM once the waves run (5.4 TB/s between the first product and the last; a kernel that only reads the same
+// weights in the same order reaches 5.8); before that stand the 128 KB of x that every CU reads (16 rows) and the code's
+// own arrival, which is why it is kept short.  us: 1 x 32000 x 4096 18.6 (floor 13.3), 16 x 128256 x 4096 63 (54),
+// 1 x 152064 x 8192 129 (126), 13 x 100003 x 2080 in groups of 32 with zero points 57 (28: four scalings per load).
 // ----------------------------------------------------------------------------------------------
 constexpr int W4S_NT = 1024;
 constexpr int W4S_WAVES = W4S_NT / 64;
 constexpr int W4S_LDS = 160 * 1024;
 constexpr int W4S_WGS = 256;
-#ifndef W4_FEW
-#define W4_FEW 8
-#define W4_RA (G == 128 ? 1 : G == 64 ? 2 : 3)
-#define W4_RB (G == 128 ? 2 : G == 64 ? 2 : 3)
-#endif
 
 template <bool I8, int G, int MT>
 struct W4StreamShape {
@@ -755,14 +761,30 @@ bool streams(const W4Args& a) {
          a.lds < ((int64_t)1 << 24) && a.ldz < ((int64_t)1 << 27);
 }
 
+// Quads on their way: 4 KB of a tile and more asks for less of the code, which every launch fetches anew: shares of
+// under eight quads are done sooner with one (1 x 32000 x 4096: 18.6 us against 19.5, 8 x 4000 x 8192: 11.1 against
+// 14.2), longer ones with two (1 x 152064 x 8192: 129 us against 132).  Quads of smaller groups are shorter.
 template <bool I8, int G, int MT>
 hipError_t stream_rows(W4Args& a, hipStream_t stream) {
-  constexpr int QUADS = W4_FEW;
-  const int64_t share = (a.N + 15) / 16 * W4StreamShape<I8, G, MT>::quads(a.K) / (W4S_WGS * W4S_WAVES);
-  if (share < QUADS) return launch_stream<I8, G, MT, W4_RA>(a, stream);
-  return launch_stream<I8, G, MT, W4_RB>(a, stream);
+  if constexpr (G == 128) {
+    const int64_t share = (a.N + 15) / 16 * W4StreamShape<I8, G, MT>::quads(a.K) / (W4S_WGS * W4S_WAVES);
+    return share < 8 ? launch_stream<I8, G, MT, 1>(a, stream) : launch_stream<I8, G, MT, 2>(a, stream);
+  } else {
+    return launch_stream<I8, G, MT, G == 64 ? 2 : 3>(a, stream);
+  }
 }
 
+// The rows decide.  Up to 32 that fit the LDS: k_w4_stream.  Else k_w4 with as many 16-row operands as the rows
+// fill, up to four, so that a weight is unpacked once for up to 64 rows; its other sizes are what the registers of
+// two waves a SIMD hold (64 x 64128 x 4096, us; "spilled": operands went through memory):
+//   bf16, 128: 2 weight tiles a wave and 256 columns a chunk 61, 4 and 128 82 (spilled)
+//   bf16, 64:  2 and 128 columns 68, 4 and 128 219 (spilled)
+//   bf16, 32:  32 rows, 2 and 256 columns 83 (103 with zero points); 64 rows, 2 and 128 75, but 431 with zero points
+//              (spilled)
+//   8 bits, 128: 4 and 256 columns 51 (128 x 8192 columns: 159 against 188 with 128); 64 and 32: 2 and 256 columns
+//              53 and 73, 4 and 128 119 and 676 (spilled)
+// Up to 16 rows that do not fit, and weights of so few rows that a workgroup of 128 of them leaves CUs idle (N below
+// 16384: 16 x 4000 x 8192 11 us against 30), the four waves share 16 weight rows and split the columns.
 template <bool I8, int G>
 hipError_t launch_rows(W4Args& a, hipStream_t stream) {
   if (streams<I8, G, 1>(a)) return stream_rows<I8, G, 1>(a, stream);
@@ -771,9 +793,12 @@ hipError_t launch_rows(W4Args& a, hipStream_t stream) {
     if (a.N < 16384) return launch<I8, G, 1, 1, 4, 512, 2, 3>(a, stream);
     return launch<I8, G, 1, 2, 1, 256, 2, 3>(a, stream);
   }
-  if (a.B <= 32) return launch<I8, G, 2, 2, 1, 256, 1, 2>(a, stream);
-  constexpr int NT = I8 && G == 128 ? 4 : 2, KC = !I8 && G < 128 ? 128 : 256;
-  return launch<I8, G, 4, NT, 1, KC, 1, 2>(a, stream);
+  constexpr bool NARROW = !I8 && G == 32;
+  if (NARROW || a.B <= 32) return launch<I8, G, 2, 2, 1, 256, 1, 2>(a, stream);
+  if constexpr (!NARROW) {
+    constexpr int NT = I8 && G == 128 ? 4 : 2, KC = !I8 && G == 64 ? 128 : 256;
+    return launch<I8, G, 4, NT, 1, KC, 1, 2>(a, stream);
+  }
 }
 
 }  // namespace
@@ -808,7 +833,7 @@ albireo_status_t albireo_matmul_w4(const void* x, albireo_rows_t x_type, int64_t
   a.scales = static_cast<const unsigned char*>(w.scales);
   a.zeros = w.zeros;
   a.out = static_cast<unsigned char*>(out);
-  a.ldx = ldx, a.ldq = w.ldq, a.lds = w.lds, a.ldz = w.ldz, a.ldo = ldo;
+  a.ldx = ldx, a.ldq = w.ldq, a.lds = w.lds, a.ldz = w.zeros ? w.ldz : 0, a.ldo = ldo;
   a.N = w.N;
   a.B = (int32_t)B, a.K = (int32_t)w.K;
   a.scale_bf16 = w.scale_dtype == ALBIREO_BF16;

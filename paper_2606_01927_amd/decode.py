@@ -65,16 +65,26 @@ def _vector(t: torch.Tensor, name: str, device, dtype, n: int) -> int:
     return t.data_ptr()
 
 
+# The current stream's handle alone: building the Stream object around it takes 2.7 of a prepared call's 6.3 us.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 class _Prepared:
     """The marshalled arguments of one call.  ``result`` is what the function of the same name returns."""
     _name = ""
 
     def _set(self, args, keep, result, stream):
         self._fn = getattr(_lib, self._name)
-        self._args, self._keep, self.result, self.stream = args, keep, result, stream
+        # as C values already, so that a call converts nothing but the stream
+        self._args = tuple(v if v is None or hasattr(v, "_obj") else t(v) for t, v in zip(self._fn.argtypes, args))
+        self._keep, self.result, self.stream = keep, result, stream
 
     def __call__(self):
-        st = self._fn(*self._args, _stream(self.stream))
+        if self.stream is None and _raw_stream is not None:
+            handle = _raw_stream(torch.cuda.current_device())
+        else:
+            handle = _stream(self.stream)
+        st = self._fn(*self._args, handle)
         if st != OK:
             raise AlbireoError(st, self._name)
         return self.result
