@@ -37,6 +37,7 @@ struct W4Args {
 //   bf16:   a byte 0x0q is, read as an 8-bit float with 4 exponent and 3 mantissa bits, q 2^-9 (denormal up to 7),
 //           and the hardware's conversion to bf16 with a scale of 2^9 gives q, two at a time.
 //   8 bits: the nibbles of a dword are two operands of four bytes, and a group's sum is an exact integer.
+//           To the signed bytes 16 (q - 8), so a zero point of 8 is there already.
 // Unpacking costs 28 (bf16) or 12 (8 bits) instructions per 16-byte load, beside 4 or 2 matrix instructions per 16
 // rows of x and 4 multiply-adds (8 bits: and conversions) per 16 rows and group.
 //
@@ -160,7 +161,8 @@ __device__ __forceinline__ void by_group(uint32_t (&d)[4]) {
   }
 }
 
-// Where the sums of group g of 128 columns start: -8 sum x, x against a constant on the matrix units.
+// -8 sum x over group g of 128 columns, x against a constant on the matrix units: where the sums of bf16 rows start,
+// and what zero points other than 8 are taken against.
 template <bool I8, int G>
 __device__ __forceinline__ u32x4 group_start(const u32x4 (&xa)[I8 ? 2 : 4], int g) {
   constexpr int GS = 128 / G;
@@ -193,7 +195,11 @@ __device__ __forceinline__ uint32_t pair_of(uint32_t b, bool high) {
               : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 512.0f, false));
 }
 
-// r[m] += the columns of group g of rows m times their weights' q.
+// The nibbles of a dword as signed bytes 16 (q - 8): the low ones (columns 0 2 4 6 of eight) and the high ones.
+__device__ __forceinline__ uint32_t low_bytes(uint32_t d) { return ((d << 4) ^ 0x80808080u) & 0xf0f0f0f0u; }
+__device__ __forceinline__ uint32_t high_bytes(uint32_t d) { return (d ^ 0x80808080u) & 0xf0f0f0f0u; }
+
+// r[m] += the columns of group g of rows m times their weights: q in bf16, 16 (q - 8) in 8 bits.
 template <bool I8, int G, int MT>
 __device__ __forceinline__ void multiply_group(u32x4 (&r)[MT], const u32x4 (&xa)[MT][I8 ? 2 : 4], const uint32_t (&d)[4], int g) {
   constexpr int GS = 128 / G;
@@ -209,7 +215,7 @@ __device__ __forceinline__ void multiply_group(u32x4 (&r)[MT], const u32x4 (&xa)
             __builtin_bit_cast(bf16x8, xa[m][i]), __builtin_bit_cast(bf16x8, wv), __builtin_bit_cast(f32x4, r[m]), 0, 0, 0));
     }
   } else if constexpr (G == 32) {
-    const uint64_t wv = (uint64_t)((d[g] >> 4) & 0x0f0f0f0fu) << 32 | (d[g] & 0x0f0f0f0fu);
+    const uint64_t wv = (uint64_t)high_bytes(d[g]) << 32 | low_bytes(d[g]);
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       const u32x4 x4 = xa[m][g >> 1];
@@ -220,8 +226,7 @@ __device__ __forceinline__ void multiply_group(u32x4 (&r)[MT], const u32x4 (&xa)
   } else {
 #pragma unroll
     for (int i = g * (2 / GS); i < (g + 1) * (2 / GS); ++i) {
-      const u32x4 wv = {d[2 * i] & 0x0f0f0f0fu, (d[2 * i] >> 4) & 0x0f0f0f0fu, d[2 * i + 1] & 0x0f0f0f0fu,
-                        (d[2 * i + 1] >> 4) & 0x0f0f0f0fu};
+      const u32x4 wv = {low_bytes(d[2 * i]), high_bytes(d[2 * i]), low_bytes(d[2 * i + 1]), high_bytes(d[2 * i + 1])};
 #pragma unroll
       for (int m = 0; m < MT; ++m)
         r[m] = __builtin_bit_cast(u32x4, __builtin_amdgcn_mfma_i32_16x16x64_i8(
@@ -235,13 +240,14 @@ __device__ __forceinline__ void multiply_group(u32x4 (&r)[MT], const u32x4 (&xa)
 //
 // A workgroup of four waves takes RN = (4 / WK) NT 16 weight rows and up to MT 16 rows of x.  A chunk of KC columns
 // of x is staged in LDS with the weights' scales and, with zero points, scale (zero - 8) / 8.  A group's sum starts at
-// -8 sum x, which the matrix units find against a constant operand (they wait for the vector instructions anyway;
-// summing x while staging it cost 256 x 152064 x 4096 8 us), so a zero point of 8 costs nothing further.  PD chunks are
-// on their way while one is multiplied: x and scales through registers into the other of two LDS buffers, one barrier
-// per chunk.  With WK = 4 the waves share their rows and each takes every fourth 128 columns, joined through LDS.
+// -8 sum x for bf16 rows, which the matrix units find against a constant operand; 8-bit rows multiply 16 (q - 8) and
+// need that sum with zero points alone.  The weights of PD chunks and the x and scales of PX are on their way while
+// one is multiplied, x and scales through registers into the other of two LDS buffers, one barrier per chunk.  With
+// WK = 4 the waves share their rows and each takes every fourth 128 columns, joined through LDS.
 //
-// 8-bit rows, us: 64 x 128256 x 8192 159 (floor 113), 256 x 152064 x 4096 311 (1.03 PFLOP/s; the same product of bf16
-// weights by the library 422).
+// us: 64 x 128256 x 8192 8-bit 160 (floor 113), bf16 220; 256 x 152064 x 4096 8-bit 310 (1.03 PFLOP/s), bf16 463 (the
+// product of unquantised bf16 weights by the library: 422).  Counters for the former: vector instructions 48 % of the
+// time, matrix units 23 %, the rest waits at barriers and for LDS that two waves a SIMD do not cover.
 // ----------------------------------------------------------------------------------------------
 template <bool I8, int G, int MT, int NT, int WK, int KC>
 struct W4Shape {
@@ -257,12 +263,12 @@ struct W4Shape {
   static_assert(XU % W4_NT == 0, "whole units per thread");
   struct Buf {
     alignas(16) unsigned char x[ROWS * XST];
-    alignas(16) float scale[NG][RN];
+    alignas(16) float scale[NG][RN];               // 8 bits: over 16
     alignas(16) float off[NG][RN];                 // with zero points: scale (zero - 8) / 8, against -8 sum x
   };
 };
 
-template <bool I8, int G, class ST, bool Z, int MT, int NT, int WK, int KC, int PD, int MW>
+template <bool I8, int G, class ST, bool Z, int MT, int NT, int WK, int KC, int PD, int PX, int MW>
 __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
   using S = W4Shape<I8, G, MT, NT, WK, KC>;
   __shared__ typename S::Buf buf[2];
@@ -335,7 +341,7 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
       const int u = t + i * W4_NT, r = u / S::NG, g = u % S::NG;
       if (S::RN * S::NG % W4_NT == 0 || r < S::RN) {
         const float sc = k0 / G + g < groups ? __uint_as_float(ST::ES == 2 ? st.s[i] << 16 : st.s[i]) : 0.0f;
-        b.scale[g][r] = sc;
+        b.scale[g][r] = I8 ? 0.0625f * sc : sc;
         if constexpr (Z) b.off[g][r] = sc * (0.125f * (float)((int)st.z[i] - 8));
       }
     }
@@ -376,14 +382,15 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
         u32x4 start[MT];
         float scale[NT];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) start[m] = group_start<I8, G>(xa[m], g);
+        for (int m = 0; m < MT; ++m)
+          if constexpr (!I8 || Z) start[m] = group_start<I8, G>(xa[m], g);
 #pragma unroll
         for (int j = 0; j < NT; ++j) scale[j] = b.scale[ks * GS + g][wn + j * 16 + c16];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
           u32x4 r[MT];
 #pragma unroll
-          for (int m = 0; m < MT; ++m) r[m] = start[m];
+          for (int m = 0; m < MT; ++m) r[m] = I8 ? u32x4{0, 0, 0, 0} : start[m];
           multiply_group<I8, G, MT>(r, xa, d[j], g);
 #pragma unroll
           for (int m = 0; m < MT; ++m)
@@ -405,29 +412,27 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
     }
   };
 
-  // PD chunks are on their way: x and scales of chunk c + PD go out as chunk c starts, its weights as chunk c's
-  // have been used, and the staging of chunk c + 1 is written to LDS at the end of chunk c.
+  // The weights of PD chunks are on their way, x and scales of PX: those of chunk c + PX go out as chunk c starts, the
+  // weights of chunk c + PD when chunk c's have been used, and the staging of chunk c + 1 is written to LDS at the end
+  // of chunk c.  Without a branch: a chunk past K loads row ends and counts as zeros, so the registers on their way
+  // are waited for at their use alone.
+  static_assert(PD % PX == 0, "one turn of the weights' registers is whole turns of the staging's");
   u32x4 wr[PD][NT][S::KS];
-  Stage st[PD];
-  static_for<PD>([&](auto I) {
-    constexpr int i = decltype(I)::value;
-    load_x(st[i], i * KC);
-    load_w(wr[i], i * KC);
-  });
+  Stage st[PX];
+  static_for<PX>([&](auto I) { load_x(st[decltype(I)::value], decltype(I)::value * KC); });
+  static_for<PD>([&](auto I) { load_w(wr[decltype(I)::value], decltype(I)::value * KC); });
   put(st[0], buf[0], 0);
   int at = 0;
-  // Without a branch: a chunk past K loads row ends and counts as zeros, so the registers on their way are waited
-  // for at their use alone.
   for (int k1 = 0; k1 < a.K; k1 += PD * KC) {
     static_for<PD>([&](auto I) {
       constexpr int i = decltype(I)::value;
       const int k0 = k1 + i * KC;
       __syncthreads();
-      load_x(st[i], k0 + PD * KC);
+      load_x(st[i % PX], k0 + PX * KC);
       multiply(wr[i], buf[at], k0);
       load_w(wr[i], k0 + PD * KC);
       at ^= 1;
-      put(st[(i + 1) % PD], buf[at], k0 + KC);
+      put(st[(i + 1) % PX], buf[at], k0 + KC);
     });
   }
 
@@ -533,8 +538,10 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
       const int u = first + i * 64 + lane;
       if (u < upr) {
         *reinterpret_cast<u32x4*>(p + u * 16) = nibble_order<I8>(xv[i]);
-        const float sum = group_sum<I8, L>(xv[i]);
-        if (lane % L == 0) sp[u / L * S::ROWS] = sum;
+        if constexpr (!I8 || Z) {
+          const float sum = group_sum<I8, L>(xv[i]);
+          if (lane % L == 0) sp[u / L * S::ROWS] = sum;
+        }
       }
     }
   };
@@ -650,12 +657,14 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) sc[e] = e < again ? 0.0f : __uint_as_float(d.s[e]);
         }
-        // the zero points' share of the four groups: one fp32 instruction, lane q4 * 16 + c16 giving group q4
-        const float s01 = (q4 & 1) ? sc[1] : sc[0], s23 = (q4 & 1) ? sc[3] : sc[2];
-        const float off = ((q4 & 2) ? s23 : s01) * (Z ? -(float)(d.z >> (8 * q4) & 0xffu) : -8.0f);
+        if constexpr (!I8 || Z) {
+          // the zero points' share of the four groups: one fp32 instruction, lane q4 * 16 + c16 giving group q4
+          const float s01 = (q4 & 1) ? sc[1] : sc[0], s23 = (q4 & 1) ? sc[3] : sc[2];
+          const float off = ((q4 & 2) ? s23 : s01) * ((I8 ? 8.0f : 0.0f) - (Z ? (float)(d.z >> (8 * q4) & 0xffu) : 8.0f));
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-          total[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(xsum[(g0 + q4) * S::ROWS + m * 16 + c16], off, total[m], 0, 0, 0);
+          for (int m = 0; m < MT; ++m)
+            total[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(xsum[(g0 + q4) * S::ROWS + m * 16 + c16], off, total[m], 0, 0, 0);
+        }
 #pragma unroll
         for (int s = 0; s < KQ; ++s) {
           u32x4 xa[MT][I8 ? 2 : 4];
@@ -669,11 +678,12 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
 #pragma unroll
             for (int m = 0; m < MT; ++m) r[m] = u32x4{0, 0, 0, 0};
             multiply_group<I8, G, MT>(r, xa, dw, g);
+            const float scale = I8 ? 0.0625f * sc[s * GS + g] : sc[s * GS + g];
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                total[m][e] = fmaf(I8 ? (float)(int)r[m][e] : __uint_as_float(r[m][e]), sc[s * GS + g], total[m][e]);
+                total[m][e] = fmaf(I8 ? (float)(int)r[m][e] : __uint_as_float(r[m][e]), scale, total[m][e]);
           }
         }
         if (++ck == nq) {
@@ -717,7 +727,7 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
   }
 }
 
-template <bool I8, int G, int MT, int NT, int WK, int KC, int PD, int MW>
+template <bool I8, int G, int MT, int NT, int WK, int KC, int PD, int PX, int MW>
 hipError_t launch(W4Args& a, hipStream_t stream) {
   using S = W4Shape<I8, G, MT, NT, WK, KC>;
   const int64_t nb = (a.N + S::RN - 1) / S::RN, mb = (a.B + S::ROWS - 1) / S::ROWS;
@@ -726,11 +736,11 @@ hipError_t launch(W4Args& a, hipStream_t stream) {
   a.m_blocks = (int32_t)mb;
   const dim3 grid((unsigned)(nb * mb)), nt(W4_NT);
   if (a.scale_bf16) {
-    if (a.zeros) hipLaunchKernelGGL((k_w4<I8, G, BF16T, true, MT, NT, WK, KC, PD, MW>), grid, nt, 0, stream, a);
-    else hipLaunchKernelGGL((k_w4<I8, G, BF16T, false, MT, NT, WK, KC, PD, MW>), grid, nt, 0, stream, a);
+    if (a.zeros) hipLaunchKernelGGL((k_w4<I8, G, BF16T, true, MT, NT, WK, KC, PD, PX, MW>), grid, nt, 0, stream, a);
+    else hipLaunchKernelGGL((k_w4<I8, G, BF16T, false, MT, NT, WK, KC, PD, PX, MW>), grid, nt, 0, stream, a);
   } else {
-    if (a.zeros) hipLaunchKernelGGL((k_w4<I8, G, F32T, true, MT, NT, WK, KC, PD, MW>), grid, nt, 0, stream, a);
-    else hipLaunchKernelGGL((k_w4<I8, G, F32T, false, MT, NT, WK, KC, PD, MW>), grid, nt, 0, stream, a);
+    if (a.zeros) hipLaunchKernelGGL((k_w4<I8, G, F32T, true, MT, NT, WK, KC, PD, PX, MW>), grid, nt, 0, stream, a);
+    else hipLaunchKernelGGL((k_w4<I8, G, F32T, false, MT, NT, WK, KC, PD, PX, MW>), grid, nt, 0, stream, a);
   }
   return hipGetLastError();
 }
@@ -776,28 +786,41 @@ hipError_t stream_rows(W4Args& a, hipStream_t stream) {
 
 // The rows decide.  Up to 32 that fit the LDS: k_w4_stream.  Else k_w4 with as many 16-row operands as the rows
 // fill, up to four, so that a weight is unpacked once for up to 64 rows; its other sizes are what the registers of
-// two waves a SIMD hold (64 x 64128 x 4096, us; "spilled": operands went through memory):
-//   bf16, 128: 2 weight tiles a wave and 256 columns a chunk 61, 4 and 128 82 (spilled)
-//   bf16, 64:  2 and 128 columns 68, 4 and 128 219 (spilled)
+// two waves a SIMD hold without spilling operands to memory (64 x 64128 x 4096, us; "spilled" where they did not):
+//   bf16, 128: 2 weight tiles a wave and 256 columns a chunk 62, 4 and 128 82 (spilled)
+//   bf16, 64:  2 and 128 columns 66, 4 and 128 219 (spilled)
 //   bf16, 32:  32 rows, 2 and 256 columns 83 (103 with zero points); 64 rows, 2 and 128 75, but 431 with zero points
 //              (spilled)
-//   8 bits, 128: 4 and 256 columns 51 (128 x 8192 columns: 159 against 188 with 128); 64 and 32: 2 and 256 columns
-//              53 and 73, 4 and 128 119 and 676 (spilled)
-// Up to 16 rows that do not fit, and weights of so few rows that a workgroup of 128 of them leaves CUs idle (N below
-// 16384: 16 x 4000 x 8192 11 us against 30), the four waves share 16 weight rows and split the columns.
+//   8 bits, 64 and 32: 2 and 256 columns 50 and 73, 4 and 128 119 and 676 (spilled)
+//   8 bits, 128: 4 and 256 columns where that makes 384 workgroups, three in four of the 512 that run at once (64 x
+//              128256 x 8192: 159 against 186 with 2), else 2 and the weights of two chunks on their way (64 x 64128 x
+//              4096: 44.5 against 50)
+// Where even workgroups of 128 weight rows are too few for the CUs, the four waves share 16 weight rows and split the
+// columns: 16 x 4000 x 8192 11 us against 30, 64 x 2000 x 4096 17 against 34 (8 bits: 12 against 24), 128 x 4000 x
+// 8192 8 bits 26 against 41.  Each such workgroup stages all of x for its 16, so with more than 16 rows it pays up to 64
+// workgroups only: 64 x 24000 x 4096 97 against 34.
 template <bool I8, int G>
 hipError_t launch_rows(W4Args& a, hipStream_t stream) {
   if (streams<I8, G, 1>(a)) return stream_rows<I8, G, 1>(a, stream);
   if (streams<I8, G, 2>(a)) return stream_rows<I8, G, 2>(a, stream);
-  if (a.B <= 16) {
-    if (a.N < 16384) return launch<I8, G, 1, 1, 4, 512, 2, 3>(a, stream);
-    return launch<I8, G, 1, 2, 1, 256, 2, 3>(a, stream);
-  }
   constexpr bool NARROW = !I8 && G == 32;
-  if (NARROW || a.B <= 32) return launch<I8, G, 2, 2, 1, 256, 1, 2>(a, stream);
+  const int64_t rows = a.B <= 16 ? 16 : a.B <= 32 || NARROW ? 32 : 64;
+  const int64_t wgs = (a.N + 127) / 128 * ((a.B + rows - 1) / rows);  // of 128 weight rows
+  const bool few = rows == 16 ? wgs < 256 : wgs <= 64;
+  if (rows == 16) {
+    if (few) return launch<I8, G, 1, 1, 4, 512, 2, 2, 3>(a, stream);
+    return launch<I8, G, 1, 2, 1, 256, 2, 2, 3>(a, stream);
+  }
+  if (rows == 32) {
+    if (few) return launch<I8, G, 2, 1, 4, 512, 1, 1, 2>(a, stream);
+    return launch<I8, G, 2, 2, 1, 256, 1, 1, 2>(a, stream);
+  }
   if constexpr (!NARROW) {
-    constexpr int NT = I8 && G == 128 ? 4 : 2, KC = !I8 && G == 64 ? 128 : 256;
-    return launch<I8, G, 4, NT, 1, KC, 1, 2>(a, stream);
+    if (few) return launch<I8, G, 4, 1, 4, 512, 1, 1, 1>(a, stream);
+    if constexpr (I8 && G == 128)
+      if ((a.N + 255) / 256 * ((a.B + 63) / 64) >= 384) return launch<I8, G, 4, 4, 1, 256, 1, 1, 2>(a, stream);
+    constexpr int KC = !I8 && G == 64 ? 128 : 256, PD = I8 && G == 128 ? 2 : 1;
+    return launch<I8, G, 4, 2, 1, KC, PD, 1, 2>(a, stream);
   }
 }
 
