@@ -36,8 +36,8 @@ struct W4Args {
 // the nibbles come out of a dword: the matrix units add over columns, so any order will do that both sides share.
 //   bf16:   a byte 0x0q is, read as an 8-bit float with 4 exponent and 3 mantissa bits, q 2^-9 (denormal up to 7),
 //           and the hardware's conversion to bf16 with a scale of 2^9 gives q, two at a time.
-//   8 bits: the nibbles of a dword are two operands of four bytes, and a group's sum is an exact integer.
-//           To the signed bytes 16 (q - 8), so a zero point of 8 is there already.
+//   8 bits: the nibbles of a dword become two operands of four signed bytes, 16 (q - 8), so a zero point of 8 is there
+//           already; a group's sum is an exact integer.
 // Unpacking costs 28 (bf16) or 12 (8 bits) instructions per 16-byte load, beside 4 or 2 matrix instructions per 16
 // rows of x and 4 multiply-adds (8 bits: and conversions) per 16 rows and group.
 //
@@ -821,6 +821,8 @@ hipError_t launch_rows(W4Args& a, hipStream_t stream) {
       if ((a.N + 255) / 256 * ((a.B + 63) / 64) >= 384) return launch<I8, G, 4, 4, 1, 256, 1, 1, 2>(a, stream);
     constexpr int KC = !I8 && G == 64 ? 128 : 256, PD = I8 && G == 128 ? 2 : 1;
     return launch<I8, G, 4, 2, 1, KC, PD, 1, 2>(a, stream);
+  } else {
+    return hipErrorInvalidValue;  // not reached: 32 rows a workgroup at most
   }
 }
 

@@ -69,15 +69,21 @@ __device__ __forceinline__ void store_values(unsigned char* p, const float (&v)[
 
 __device__ __forceinline__ uint32_t q_byte(float v) { return (uint32_t)(int)rintf(v) & 0xffu; }
 
-// sum of a double over the wave's lanes, combined in the order of wave_sum
+// sum of a double over the wave's lanes, the same in every lane
 __device__ __forceinline__ double wave_sum_d(double v) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-  return v;
+  const auto bits = [](double d) { return __builtin_bit_cast(uint64_t, d); };
+  const auto value = [](uint64_t b) { return __builtin_bit_cast(double, b); };
+  v += value(dpp_mov64<DPP_ROW_SHR + 1>(bits(v)));
+  v += value(dpp_mov64<DPP_ROW_SHR + 2>(bits(v)));
+  v += value(dpp_mov64<DPP_ROW_SHR + 4>(bits(v)));
+  v += value(dpp_mov64<DPP_ROW_SHR + 8>(bits(v)));
+  v += value(dpp_mov64<DPP_ROW_BCAST15, 0xa>(bits(v)));
+  v += value(dpp_mov64<DPP_ROW_BCAST31, 0xc>(bits(v)));
+  return value(lane_u64(bits(v), 63));
 }
 
 // A row is held in registers by TPR threads, SPT slots of 16 bytes of its type each (8 bf16 or 4 fp32): 64
-// threads (a wave, without a barrier) for short rows, else a workgroup of 256 or 1024.  Every input is read
+// threads (a wave, without a barrier) for short rows, else a workgroup of 256 to 1024.  Every input is read
 // once and every output written once; the loads of a row all go out before the first is used (a slot past the
 // row's last reloads that one and counts as zeros).  Rows need no alignment past the element's, so odd widths
 // and strides keep the wide accesses; the values behind the last whole slot are one each for the first threads.
@@ -86,7 +92,9 @@ __device__ __forceinline__ double wave_sum_d(double v) {
 // sum of a row's thousands of squares is off by a unit or two, and with it would be whether an 8-bit value
 // next to the middle of two steps goes up or down.  A sum that leaves fp32 stays in double.
 //
-// Bound: HBM.
+// Bound: HBM, 5.4-5.8 TB/s for a prompt's rows (8192 x 4096 bf16 with the residual 46 us; a large copy reaches 5.1),
+// and for few rows the chain of load, two reductions and store: 1 x 4096 2.4 us, 256 x 8192 to 8 bits 5.5 us (2.9 at
+// the rate of a copy), 1000 x 5121 fp32 to both outputs 13.3 (9.0).
 template <class DT, class WT, int TPR, int SPT>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormArgs a) {
   constexpr int VEC = DT::VEC, ES = DT::ES, NW = TPR / 64;
@@ -202,6 +210,10 @@ void launch(const NormArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL((k_norm<DT, WT, TPR, SPT>), dim3((unsigned)grid), dim3(TPR < 256 ? 256 : TPR), 0, stream, a);
 }
 
+// The narrowest workgroup whose threads hold a row in few slots each: 64 threads cost no barrier, and several small
+// workgroups on a CU overlap one row's reductions with another's loads (1000 x 5121 fp32: 13.3 us on 512 threads, 14.9 on
+// 1024).  Rows of 513 to 1024 slots that leave a CU alone with one or two take 1024 threads for 256 (256 x 8192 bf16 to 8
+// bits: 5.5 us against 5.9; with 1000 rows 12.4 against 10.7).
 template <class DT, class WT>
 void launch_width(const NormArgs& a, hipStream_t stream) {
   const int slots = (a.D + DT::VEC - 1) / DT::VEC;
@@ -209,7 +221,9 @@ void launch_width(const NormArgs& a, hipStream_t stream) {
   else if (slots <= 128) launch<DT, WT, 64, 2>(a, stream);
   else if (slots <= 256) launch<DT, WT, 256, 1>(a, stream);
   else if (slots <= 512) launch<DT, WT, 256, 2>(a, stream);
+  else if (slots <= 1024 && a.T <= 512) launch<DT, WT, 1024, 1>(a, stream);
   else if (slots <= 1024) launch<DT, WT, 256, 4>(a, stream);
+  else if (slots <= 1536) launch<DT, WT, 512, 3>(a, stream);
   else if (slots <= 2048) launch<DT, WT, 1024, 2>(a, stream);
   else if (slots <= 4096) launch<DT, WT, 1024, 4>(a, stream);
   else if constexpr (DT::VEC == 4) launch<DT, WT, 1024, 8>(a, stream);
