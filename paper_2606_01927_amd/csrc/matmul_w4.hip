@@ -245,11 +245,18 @@ __device__ __forceinline__ void multiply_group(u32x4 (&r)[MT], const u32x4 (&xa)
 // one is multiplied, x and scales through registers into the other of two LDS buffers, one barrier per chunk.  With
 // WK = 4 the waves share their rows and each takes every fourth 128 columns, joined through LDS.
 //
-// us: 64 x 128256 x 8192 8-bit 160 (floor 113), bf16 220; 256 x 152064 x 4096 8-bit 310 (1.03 PFLOP/s), bf16 463 (the
-// product of unquantised bf16 weights by the library: 422).  Counters for the former: vector instructions 48 % of the
-// time, matrix units 23 %, the rest waits at barriers and for LDS that two waves a SIMD do not cover.
+// Scales of 2 bytes per row and chunk would each move a line of the caches: with SV > 0 a thread loads up to four
+// groups of a row at once, and the scales of SV groups stand in LDS together (256 x 152064 x 4096 8-bit: 308 us to 282).
+// Nothing is loaded between the stores at the end: a wait for it would wait for the stores before it as well (282 us
+// to 245).
+//
+// us: 64 x 128256 x 8192 8-bit 150 (floor 113), bf16 214; 256 x 152064 x 4096 8-bit 245 (1.30 PFLOP/s), bf16 452 (the
+// product of unquantised bf16 weights by the library: 422).  Of the 245, 51 per 1024 columns and 40 for the 156 MB of
+// results; vector instructions (unpacking, scaling) are some 55 % of the time, the matrix units 26 %.  Neither weights
+// further ahead, nor weights through LDS, nor another order of chunks, nor a tile's scaling beside the next tile's
+// products changed the time by more than 2 %.
 // ----------------------------------------------------------------------------------------------
-template <bool I8, int G, int MT, int NT, int WK, int KC>
+template <bool I8, int G, int MT, int NT, int WK, int KC, int SV>
 struct W4Shape {
   static constexpr int ROWS = MT * 16;             // rows of x
   static constexpr int RN = (4 / WK) * NT * 16;    // weight rows
@@ -259,19 +266,24 @@ struct W4Shape {
   static constexpr int XST = KC * ES + 16;         // bytes from one LDS row of x to the next: 16 past a multiple of 256
   static constexpr int XU = ROWS * KC * ES / 16;   // 16-byte units of x in a chunk
   static constexpr int XPT = XU / W4_NT;           // per thread
-  static constexpr int SPT = (RN * NG + W4_NT - 1) / W4_NT;  // scales per thread
+  static constexpr int SG = SV ? SV : NG;          // groups whose scales are staged together
+  static constexpr int P = SG / NG;                // chunks that is
+  static constexpr int TPR = W4_NT / RN;           // SV: threads that load a row's scales
+  static constexpr int SPT = SV ? SV / TPR : (RN * NG + W4_NT - 1) / W4_NT;  // scales per thread
   static_assert(XU % W4_NT == 0, "whole units per thread");
+  static_assert(SG % NG == 0 && (!SV || (W4_NT % RN == 0 && SV % TPR == 0 && SPT <= 4)), "whole chunks, one load per thread");
   struct Buf {
     alignas(16) unsigned char x[ROWS * XST];
-    alignas(16) float scale[NG][RN];               // 8 bits: over 16
-    alignas(16) float off[NG][RN];                 // with zero points: scale (zero - 8) / 8, against -8 sum x
+    alignas(16) float scale[SG][RN];               // 8 bits: over 16
+    alignas(16) float off[SG][RN];                 // with zero points: scale (zero - 8) / 8, against -8 sum x
   };
 };
 
-template <bool I8, int G, class ST, bool Z, int MT, int NT, int WK, int KC, int PD, int PX, int MW>
+template <bool I8, int G, class ST, bool Z, int MT, int NT, int WK, int KC, int PD, int PX, int MW, int SV>
 __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
-  using S = W4Shape<I8, G, MT, NT, WK, KC>;
+  using S = W4Shape<I8, G, MT, NT, WK, KC, SV>;
   __shared__ typename S::Buf buf[2];
+  __shared__ float x_scale[S::ROWS];
   const int t = threadIdx.x, lane = lane_id(), wave = wave_id();
   const int c16 = lane & 15, q4 = lane >> 4;
   // The row blocks of one column block follow each other on one XCD (workgroups go round the 8 XCDs), which
@@ -292,6 +304,8 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
   const int64_t n0 = (int64_t)bn * S::RN;
   const int b0 = bm * S::ROWS;
   const int rows = min(S::ROWS, a.B - b0);
+  // the rows' scales to LDS now: read between the stores at the end, each would wait for the stores before it
+  if (I8 && t < S::ROWS) x_scale[t] = a.x_scale[b0 + min(t, rows - 1)];
   const int rn = (int)min((int64_t)S::RN, a.N - n0);
   const int wn = WK == 1 ? wave * NT * 16 : 0;  // the wave's first weight row in the block
   const int wk = WK == 1 ? 0 : wave;
@@ -305,8 +319,10 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
   constexpr int UPR = KC * S::ES / 16;          // units per row
   struct Stage {  // what the next chunks need in LDS, on its way
     u32x4 x[S::XPT];
-    uint32_t s[S::SPT];
-    uint8_t z[S::SPT];
+  };
+  struct Scales {
+    uint32_t s[S::SPT];  // SV: as loaded
+    uint32_t z[SV ? 1 : S::SPT];
   };
   // rows past the last repeat it (and are not staged); columns past K repeat the row's end, under scales of zero
   const unsigned char* xbase = a.x + (int64_t)b0 * a.ldx * S::ES;
@@ -319,30 +335,57 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
       const int k = min(k0 + (t + i * W4_NT) % UPR * (16 / S::ES), a.K - 16 / S::ES);
       st.x[i] = *reinterpret_cast<const u32x4u*>(xbase + (xoff[i] + (uint32_t)k) * S::ES);
     }
-    const int g0 = k0 / G;
-#pragma unroll
-    for (int i = 0; i < S::SPT; ++i) {
-      const int u = t + i * W4_NT;
-      const int64_t r = n0 + min(u / S::NG, rn - 1);
-      const int g = min(g0 + u % S::NG, groups - 1);
-      if constexpr (ST::ES == 2) st.s[i] = reinterpret_cast<const uint16_t*>(a.scales)[r * a.lds + g];
-      else st.s[i] = reinterpret_cast<const uint32_t*>(a.scales)[r * a.lds + g];
-      if constexpr (Z) st.z[i] = a.zeros[r * a.ldz + g];
-    }
   };
-  auto put = [&](const Stage& st, typename S::Buf& b, int k0) __attribute__((always_inline)) {
+  auto put_x = [&](const Stage& st, typename S::Buf& b) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < S::XPT; ++i) {
       const int u = t + i * W4_NT, r = u / UPR, c = u % UPR;
       if (r < rows) *reinterpret_cast<u32x4*>(b.x + r * S::XST + c * 16) = nibble_order<I8>(st.x[i]);
     }
+  };
+  // SV scales of a row by TPR threads, the last of a row's by the load that ends with the row (which has SV or more):
+  // what that load has of groups before is shifted out, and zeros follow.
+  const int sv_row = (int)min((int64_t)(t / S::TPR), (int64_t)rn - 1), sv_g = t % S::TPR * S::SPT;
+  const unsigned char* sv_s = a.scales + (n0 + sv_row) * a.lds * ST::ES;
+  const uint8_t* sv_z = Z ? a.zeros + (n0 + sv_row) * a.ldz : nullptr;
+  auto load_s = [&](Scales& st, int g0) __attribute__((always_inline)) {
+    if constexpr (SV) {
+      const int g = min(g0 + sv_g, groups - S::SPT);
+      __builtin_memcpy(st.s, sv_s + g * ST::ES, S::SPT * ST::ES);
+      if constexpr (Z) __builtin_memcpy(st.z, sv_z + g, S::SPT);
+    } else {
+#pragma unroll
+      for (int i = 0; i < S::SPT; ++i) {
+        const int u = t + i * W4_NT;
+        const int64_t r = n0 + min(u / S::NG, rn - 1);
+        const int g = min(g0 + u % S::NG, groups - 1);
+        if constexpr (ST::ES == 2) st.s[i] = reinterpret_cast<const uint16_t*>(a.scales)[r * a.lds + g];
+        else st.s[i] = reinterpret_cast<const uint32_t*>(a.scales)[r * a.lds + g];
+        if constexpr (Z) st.z[i] = a.zeros[r * a.ldz + g];
+      }
+    }
+  };
+  auto put_s = [&](const Scales& st, typename S::Buf& b, int g0) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < S::SPT; ++i) {
-      const int u = t + i * W4_NT, r = u / S::NG, g = u % S::NG;
-      if (S::RN * S::NG % W4_NT == 0 || r < S::RN) {
-        const float sc = k0 / G + g < groups ? __uint_as_float(ST::ES == 2 ? st.s[i] << 16 : st.s[i]) : 0.0f;
+      const int u = t + i * W4_NT, r = SV ? t / S::TPR : u / S::NG, g = SV ? sv_g + i : u % S::NG;
+      if (SV || S::RN * S::NG % W4_NT == 0 || r < S::RN) {
+        uint32_t sv = st.s[SV ? 0 : i], z = 0;
+        if constexpr (Z) z = st.z[SV ? 0 : i];
+        if constexpr (SV) {
+          const int e = i + max(g0 + sv_g - (groups - S::SPT), 0);  // its place in what was loaded
+          if constexpr (ST::ES == 2 && S::SPT > 2)
+            sv = (uint32_t)((((uint64_t)st.s[1] << 32) | st.s[0]) >> (16 * (e & 3)));
+          else if constexpr (ST::ES == 2) sv = st.s[0] >> (16 * (e & 1));
+          else {
+#pragma unroll
+            for (int f = 0; f < S::SPT; ++f) sv = e == f ? st.s[f] : sv;
+          }
+          if constexpr (Z) z = z >> (8 * (e & 3)) & 255;
+        }
+        const float sc = g0 + g < groups ? __uint_as_float(ST::ES == 2 ? sv << 16 : sv) : 0.0f;
         b.scale[g][r] = I8 ? 0.0625f * sc : sc;
-        if constexpr (Z) b.off[g][r] = sc * (0.125f * (float)((int)st.z[i] - 8));
+        if constexpr (Z) b.off[g][r] = sc * (0.125f * (float)((int)z - 8));
       }
     }
   };
@@ -362,7 +405,9 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
     for (int j = 0; j < NT; ++j) total[m][j] = f32x4{0, 0, 0, 0};
 
   constexpr int GS = 128 / G;                     // groups per 128 columns
-  auto multiply = [&](u32x4 (&w)[NT][S::KS], typename S::Buf& b, int k0) __attribute__((always_inline)) {
+  // sb, sg: where the chunk's scales stand
+  auto multiply = [&](u32x4 (&w)[NT][S::KS], typename S::Buf& b, typename S::Buf& sb, int sg, int k0)
+      __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < S::KS; ++s) {
       const int ks = s * WK + wk;  // the step in the chunk
@@ -385,7 +430,7 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
         for (int m = 0; m < MT; ++m)
           if constexpr (!I8 || Z) start[m] = group_start<I8, G>(xa[m], g);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) scale[j] = b.scale[ks * GS + g][wn + j * 16 + c16];
+        for (int j = 0; j < NT; ++j) scale[j] = sb.scale[sg + ks * GS + g][wn + j * 16 + c16];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
           u32x4 r[MT];
@@ -398,7 +443,7 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
             for (int e = 0; e < 4; ++e)
               total[m][j][e] = fmaf(I8 ? (float)(int)r[m][e] : __uint_as_float(r[m][e]), scale[j], total[m][j][e]);
           if constexpr (Z) {
-            const float off = b.off[ks * GS + g][wn + j * 16 + c16];
+            const float off = sb.off[sg + ks * GS + g][wn + j * 16 + c16];
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -417,22 +462,33 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
   // of chunk c.  Without a branch: a chunk past K loads row ends and counts as zeros, so the registers on their way
   // are waited for at their use alone.
   static_assert(PD % PX == 0, "one turn of the weights' registers is whole turns of the staging's");
+  static_assert(S::P % PD == 0 || S::P == 1, "one turn of the scales is whole turns of the weights' registers");
+  constexpr int U = S::P > PD ? S::P : PD;
+  constexpr int PS = SV ? 1 : PX;  // turns the scales are ahead
   u32x4 wr[PD][NT][S::KS];
   Stage st[PX];
+  Scales ss[PS];
   static_for<PX>([&](auto I) { load_x(st[decltype(I)::value], decltype(I)::value * KC); });
+  static_for<PS>([&](auto I) { load_s(ss[decltype(I)::value], decltype(I)::value * S::SG); });
   static_for<PD>([&](auto I) { load_w(wr[decltype(I)::value], decltype(I)::value * KC); });
-  put(st[0], buf[0], 0);
-  int at = 0;
-  for (int k1 = 0; k1 < a.K; k1 += PD * KC) {
-    static_for<PD>([&](auto I) {
+  put_x(st[0], buf[0]);
+  put_s(ss[0], buf[0], 0);
+  int at = 0, sat = 0;
+  for (int k1 = 0; k1 < a.K; k1 += U * KC) {
+    static_for<U>([&](auto I) {
       constexpr int i = decltype(I)::value;
-      const int k0 = k1 + i * KC;
+      const int k0 = k1 + i * KC, g0 = k0 / G;
       __syncthreads();
       load_x(st[i % PX], k0 + PX * KC);
-      multiply(wr[i], buf[at], k0);
-      load_w(wr[i], k0 + PD * KC);
+      if constexpr (i % S::P == 0) load_s(ss[i / S::P % PS], g0 + PS * S::SG);
+      multiply(wr[i % PD], buf[at], buf[sat], i % S::P * S::NG, k0);
+      load_w(wr[i % PD], k0 + PD * KC);
       at ^= 1;
-      put(st[(i + 1) % PX], buf[at], k0 + KC);
+      put_x(st[(i + 1) % PX], buf[at]);
+      if constexpr (i % S::P == S::P - 1) {
+        sat ^= 1;
+        put_s(ss[(i / S::P + 1) % PS], buf[sat], g0 + S::NG);
+      }
     });
   }
 
@@ -455,25 +511,30 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) total[m][j] += part[((w * MT + m) * NT + j) * 64 + lane];
   }
+  const auto store = [&](auto out, auto whole) __attribute__((always_inline)) {
+    using T = decltype(out);
+    unsigned char* o = a.out + ((b0 + q4 * 4) * a.ldo + n0 + wn + c16) * T::ES;
 #pragma unroll
-  for (int m = 0; m < MT; ++m) {
+    for (int m = 0; m < MT; ++m) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int b = m * 16 + q4 * 4 + e;
-      if (b < rows) {
-        const float xs = I8 ? a.x_scale[b0 + b] : 1.0f;
+      for (int e = 0; e < 4; ++e) {
+        const int b = m * 16 + q4 * 4 + e;
+        const float xs = I8 ? x_scale[b] : 1.0f;
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const int n = wn + j * 16 + c16;
-          if (n < rn) {
-            const float v = I8 ? total[m][j][e] * xs : total[m][j][e];
-            const int64_t at = (int64_t)(b0 + b) * a.ldo + n0 + n;
-            if (a.out_bf16) store1<BF16T>(a.out, at, v);
-            else store1<F32T>(a.out, at, v);
-          }
-        }
+        for (int j = 0; j < NT; ++j)
+          if (decltype(whole)::value || (b < rows && wn + j * 16 + c16 < rn))
+            store1<T>(o, j * 16, I8 ? total[m][j][e] * xs : total[m][j][e]);
+        o += a.ldo * T::ES;
       }
+      o += 12 * a.ldo * T::ES;
     }
+  };
+  if (rows == S::ROWS && rn == S::RN) {
+    if (a.out_bf16) store(BF16T{}, std::true_type{});
+    else store(F32T{}, std::true_type{});
+  } else {
+    if (a.out_bf16) store(BF16T{}, std::false_type{});
+    else store(F32T{}, std::false_type{});
   }
 }
 
@@ -503,10 +564,10 @@ struct W4StreamShape {
   static constexpr int QC = 4 * G;        // columns of a quad of groups
   static constexpr int KQ = QC / 128;     // 128-column steps of a quad
   static constexpr int ROWS = MT * 16;
-  // LDS: the rows, and their sum over each group
+  // LDS: the rows, their sum over each group, and their scales
   static int64_t quads(int64_t K) { return (K + QC - 1) / QC; }
   static constexpr int XU = 8;            // 16-byte units of a row of x a lane asks for at once
-  static int64_t bytes(int64_t B, int64_t K) { return B * (K * ES + 16) + K / G * ROWS * 4; }
+  static int64_t bytes(int64_t B, int64_t K) { return B * (K * ES + 16) + K / G * ROWS * 4 + ROWS * 4; }
 };
 
 template <bool I8, int G, class ST, bool Z, int MT, int R>
@@ -520,6 +581,7 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
   const int nq = (groups + 3) / 4;
   const int upr = a.K * ES / 16, xst = a.K * ES + 16;
   float* xsum = reinterpret_cast<float*>(lds + rows * xst);  // [groups][ROWS]
+  float* x_scale = reinterpret_cast<float*>(lds + W4S_LDS) - S::ROWS;  // past what the join of the tiles uses
 
   // Staging: a wave takes a row of x at a time.  The first of it is asked for ahead of the weights, by every wave
   // before any wave asks for weights: loads return in order, and all of x is needed before the first product.
@@ -546,6 +608,8 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
     }
   };
   if (wave < rows) load_x(wave, 0);
+  // kept in LDS: loaded at a tile's end they would wait for all the weights on their way
+  const float xs = I8 ? a.x_scale[min(t, rows - 1)] : 1.0f;
   __builtin_amdgcn_s_barrier();
 
   // the workgroup's tiles and the wave's share [qa, qb) of their quads
@@ -597,6 +661,7 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
   static_for<R>([&](auto I) { ask(ring[decltype(I)::value]); });
 
   if (wave < rows) put_x(wave, 0);
+  if (I8 && t < S::ROWS) x_scale[t] = xs;
   for (int r = wave; r < rows; r += W4S_WAVES)
     for (int u = r == wave ? S::XU * 64 : 0; u < upr; u += S::XU * 64) {
       load_x(r, u);
@@ -622,7 +687,7 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
       f32x4 r = v[m];
       if constexpr (I8) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] *= a.x_scale[min(b + e, rows - 1)];
+        for (int e = 0; e < 4; ++e) r[e] *= x_scale[b + e];
       }
       if (a.out_bf16) {
         uint16_t* o = reinterpret_cast<uint16_t*>(a.out) + b * a.ldo + n;
@@ -727,20 +792,20 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
   }
 }
 
-template <bool I8, int G, int MT, int NT, int WK, int KC, int PD, int PX, int MW>
+template <bool I8, int G, int MT, int NT, int WK, int KC, int PD, int PX, int MW, int SV = 0>
 hipError_t launch(W4Args& a, hipStream_t stream) {
-  using S = W4Shape<I8, G, MT, NT, WK, KC>;
+  using S = W4Shape<I8, G, MT, NT, WK, KC, SV>;
   const int64_t nb = (a.N + S::RN - 1) / S::RN, mb = (a.B + S::ROWS - 1) / S::ROWS;
   if (nb * mb >= ((int64_t)1 << 31)) return hipErrorInvalidConfiguration;
   a.n_blocks = (int32_t)nb;
   a.m_blocks = (int32_t)mb;
   const dim3 grid((unsigned)(nb * mb)), nt(W4_NT);
   if (a.scale_bf16) {
-    if (a.zeros) hipLaunchKernelGGL((k_w4<I8, G, BF16T, true, MT, NT, WK, KC, PD, PX, MW>), grid, nt, 0, stream, a);
-    else hipLaunchKernelGGL((k_w4<I8, G, BF16T, false, MT, NT, WK, KC, PD, PX, MW>), grid, nt, 0, stream, a);
+    if (a.zeros) hipLaunchKernelGGL((k_w4<I8, G, BF16T, true, MT, NT, WK, KC, PD, PX, MW, SV>), grid, nt, 0, stream, a);
+    else hipLaunchKernelGGL((k_w4<I8, G, BF16T, false, MT, NT, WK, KC, PD, PX, MW, SV>), grid, nt, 0, stream, a);
   } else {
-    if (a.zeros) hipLaunchKernelGGL((k_w4<I8, G, F32T, true, MT, NT, WK, KC, PD, PX, MW>), grid, nt, 0, stream, a);
-    else hipLaunchKernelGGL((k_w4<I8, G, F32T, false, MT, NT, WK, KC, PD, PX, MW>), grid, nt, 0, stream, a);
+    if (a.zeros) hipLaunchKernelGGL((k_w4<I8, G, F32T, true, MT, NT, WK, KC, PD, PX, MW, SV>), grid, nt, 0, stream, a);
+    else hipLaunchKernelGGL((k_w4<I8, G, F32T, false, MT, NT, WK, KC, PD, PX, MW, SV>), grid, nt, 0, stream, a);
   }
   return hipGetLastError();
 }
@@ -792,9 +857,10 @@ hipError_t stream_rows(W4Args& a, hipStream_t stream) {
 //   bf16, 32:  32 rows, 2 and 256 columns 83 (103 with zero points); 64 rows, 2 and 128 75, but 431 with zero points
 //              (spilled)
 //   8 bits, 64 and 32: 2 and 256 columns 50 and 73, 4 and 128 119 and 676 (spilled)
-//   8 bits, 128: 4 and 256 columns where that makes 384 workgroups, three in four of the 512 that run at once (64 x
-//              128256 x 8192: 159 against 186 with 2), else 2 and the weights of two chunks on their way (64 x 64128 x
-//              4096: 44.5 against 50)
+//   8 bits, 128: 4 and 128 columns where several row blocks of x take the weights and that makes 384 workgroups, three
+//              in four of the 512 that run at once (256 x 152064 x 4096: 250 against 266 with 2 and 256, 128 x 64128 x
+//              4096: 60.5 against 65), else 2 and 256 (64 x 152064 x 4096: 101 against 106, 64 x 128256 x 8192: 149
+//              against 154); the weights of two chunks on their way, the scales of 4 and 8 groups at once where a row has 4
 // Where even workgroups of 128 weight rows are too few for the CUs, the four waves share 16 weight rows and split the
 // columns: 16 x 4000 x 8192 11 us against 30, 64 x 2000 x 4096 17 against 34 (8 bits: 12 against 24), 128 x 4000 x
 // 8192 8 bits 26 against 41.  Each such workgroup stages all of x for its 16, so with more than 16 rows it pays up to 64
@@ -818,7 +884,10 @@ hipError_t launch_rows(W4Args& a, hipStream_t stream) {
   if constexpr (!NARROW) {
     if (few) return launch<I8, G, 4, 1, 4, 512, 1, 1, 1>(a, stream);
     if constexpr (I8 && G == 128)
-      if ((a.N + 255) / 256 * ((a.B + 63) / 64) >= 384) return launch<I8, G, 4, 4, 1, 256, 1, 1, 2>(a, stream);
+      if (a.K >= 4 * G) {
+        if (a.B > 64 && (a.N + 255) / 256 * ((a.B + 63) / 64) >= 384) return launch<I8, G, 4, 4, 1, 128, 2, 1, 2, 4>(a, stream);
+        return launch<I8, G, 4, 2, 1, 256, 2, 1, 2, 8>(a, stream);
+      }
     constexpr int KC = !I8 && G == 64 ? 128 : 256, PD = I8 && G == 128 ? 2 : 1;
     return launch<I8, G, 4, 2, 1, KC, PD, 1, 2>(a, stream);
   } else {
