@@ -31,7 +31,7 @@ struct W4Args {
 // The mathematics.  With W = s (q - z), one scale s and zero point z to a group of columns,
 //     sum_k x W = sum over the groups of  s (sum x q - z sum x),
 // so the matrix units multiply x by the bare 4-bit values and a scale is applied once per output and group.  Weights
-// are the B operand, straight from memory to registers: a lane loads 16 bytes, 32 columns of one weight row, so the
+// are the B operand, from memory to registers without LDS: a lane loads 16 bytes, 32 columns of one weight row, so the
 // 64 lanes of a load cover 16 rows by 128 columns.  x is the A operand, from LDS, its columns reordered to the order
 // the nibbles come out of a dword: the matrix units add over columns, so any order will do that both sides share.
 //   bf16:   a byte 0x0q is, read as an 8-bit float with 4 exponent and 3 mantissa bits, q 2^-9 (denormal up to 7),
@@ -49,9 +49,6 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(1)));  // gfx950 takes unaligned vector loads
-typedef uint32_t u32x2a2 __attribute__((ext_vector_type(2), aligned(2)));
-typedef uint32_t u32x4a4 __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t u32a1 __attribute__((aligned(1)));
 
 constexpr int W4_NT = 256;  // threads per workgroup
 
@@ -139,6 +136,10 @@ __device__ __forceinline__ void load_rows(u32x4 (&xa)[I8 ? 2 : 4], const unsigne
     }
   }
 }
+
+// the value that lane at / 4 holds
+__device__ __forceinline__ uint32_t from_lane(int at, uint32_t v) { return (uint32_t)__builtin_amdgcn_ds_bpermute(at, (int)v); }
+__device__ __forceinline__ float from_lane(int at, float v) { return __uint_as_float(from_lane(at, __float_as_uint(v))); }
 
 // The four dwords a lane loads are 32 columns, so with groups of 64 or 32 the lanes of one load hold different
 // groups: swaps between lanes put each group's columns into the same registers (two, or one).
@@ -550,8 +551,11 @@ __global__ __launch_bounds__(W4_NT, MW) void k_w4(W4Args a) {
 //
 // Bound: HBM once the waves run (5.4 TB/s between the first product and the last; a kernel that only reads the same
 // weights in the same order reaches 5.8); before that stand the 128 KB of x that every CU reads (16 rows) and the code's
-// own arrival, which is why it is kept short.  us: 1 x 32000 x 4096 18.6 (floor 13.3), 16 x 128256 x 4096 63 (54),
-// 1 x 152064 x 8192 129 (126), 13 x 100003 x 2080 in groups of 32 with zero points 57 (28: four scalings per load).
+// own arrival, which is why it is kept short.  Loads in the order of the matrix operands, a lane's 16 bytes in another
+// row than its neighbour's, took four times the cycles of the first cache (with groups of 32 four in five of all) and
+// 2-5 % more time, 34 % at 5 x 1500 x 2016; exchanging what was loaded between lanes costs less.  us: 1 x 32000 x 4096
+// 16.9 (floor 13.3), 16 x 128256 x 4096 61.6 (54), 1 x 152064 x 8192 126 (126), 13 x 100003 x 2080 in groups of 32 with
+// zero points 54 (28: waves wait for the issue of instructions, of which 130 go to a kilobyte of weights).
 // ----------------------------------------------------------------------------------------------
 constexpr int W4S_NT = 1024;
 constexpr int W4S_WAVES = W4S_NT / 64;
@@ -619,18 +623,23 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
   const uint32_t qa = nquads * wave / W4S_WAVES, qb = nquads * (wave + 1) / W4S_WAVES;
   const uint32_t ta = qa / (uint32_t)nq;
 
+  // Loads are by rows, four neighbouring lanes taking 64 bytes of one, or its four scales: the caches serve so many
+  // bytes of a line at once, and one lane's 16 bytes if the next lane is in another row.  What the matrix units want
+  // in a lane comes from lane turn / 4.
   struct Quad {
     u32x4 w[KQ];
-    uint32_t s[ST::ES == 2 ? 2 : 4];
-    uint32_t z;
+    uint32_t s, z;
   };
+  const int turn = c16 * 16 + q4 * 4;
   Quad ring[R];
   // The next quad to ask for.  The last tile is the last 16 rows whatever N is (and stores those past the tile
   // before), so a lane's distance from its tile's first row never changes; past the share's end the asking goes on
   // into the next wave's quads, and past the last tile it stays there.
   uint32_t pt = t0 + ta;
   int pk = (int)(qa - ta * nq);
-  const uint32_t wlane = c16 * (uint32_t)a.ldq + q4 * 16, slane = c16 * (uint32_t)a.lds * ST::ES, zlane = c16 * (uint32_t)a.ldz;
+  const uint32_t lrow = lane >> 2, lpart = lane & 3;
+  const uint32_t wlane = lrow * (uint32_t)a.ldq + lpart * 16, slane = (lrow * (uint32_t)a.lds + lpart) * ST::ES;
+  const uint32_t zlane = lrow * (uint32_t)a.ldz + lpart;
   int64_t prow = min((int64_t)pt * 16, a.N - 16);
   const uint8_t* wtile = a.q + prow * a.ldq;
   const unsigned char* stile = a.scales + prow * a.lds * ST::ES;
@@ -642,14 +651,9 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
 #pragma unroll
     for (int s = 0; s < KQ; ++s) d.w[s] = *reinterpret_cast<const u32x4u*>(wr + wlane + s * 64);
     const unsigned char* sr = stile + g * ST::ES;
-    if constexpr (ST::ES == 2) {
-      const u32x2a2 v = *reinterpret_cast<const u32x2a2*>(sr + slane);
-      d.s[0] = v.x, d.s[1] = v.y;
-    } else {
-      const u32x4a4 v = *reinterpret_cast<const u32x4a4*>(sr + slane);
-      d.s[0] = v.x, d.s[1] = v.y, d.s[2] = v.z, d.s[3] = v.w;
-    }
-    if constexpr (Z) d.z = *reinterpret_cast<const u32a1*>(ztile + g + zlane);
+    if constexpr (ST::ES == 2) d.s = *reinterpret_cast<const uint16_t*>(sr + slane);
+    else d.s = *reinterpret_cast<const uint32_t*>(sr + slane);
+    if constexpr (Z) d.z = (ztile + g)[zlane];
     if (++pk == nq) {
       pk = 0;
       prow = min((int64_t)++pt * 16, a.N - 16);
@@ -710,22 +714,13 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
       if (q + i < qb) {
         Quad& d = ring[i];
         const int g0 = min(ck * 4, groups - 4), again = ck * 4 - g0;  // first group, and how many the quad before had
-        float sc[4];
-        if constexpr (ST::ES == 2) {
-          uint64_t s = (uint64_t)d.s[1] << 32 | d.s[0];
-          if (again) s &= ~(uint64_t)0 << (16 * again);
-          sc[0] = __uint_as_float((uint32_t)s << 16);
-          sc[1] = __uint_as_float((uint32_t)s & 0xffff0000u);
-          sc[2] = __uint_as_float((uint32_t)(s >> 32) << 16);
-          sc[3] = __uint_as_float((uint32_t)(s >> 32) & 0xffff0000u);
-        } else {
+        const float own = (int)lpart < again ? 0.0f : __uint_as_float(ST::ES == 2 ? d.s << 16 : d.s);
+        float sc[4];  // 8 bits: over 16
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc[e] = e < again ? 0.0f : __uint_as_float(d.s[e]);
-        }
+        for (int e = 0; e < 4; ++e) sc[e] = from_lane(c16 * 16 + e * 4, I8 ? 0.0625f * own : own);
         if constexpr (!I8 || Z) {
           // the zero points' share of the four groups: one fp32 instruction, lane q4 * 16 + c16 giving group q4
-          const float s01 = (q4 & 1) ? sc[1] : sc[0], s23 = (q4 & 1) ? sc[3] : sc[2];
-          const float off = ((q4 & 2) ? s23 : s01) * ((I8 ? 8.0f : 0.0f) - (Z ? (float)(d.z >> (8 * q4) & 0xffu) : 8.0f));
+          const float off = from_lane(turn, own * ((I8 ? 8.0f : 0.0f) - (Z ? (float)d.z : 8.0f)));
 #pragma unroll
           for (int m = 0; m < MT; ++m)
             total[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(xsum[(g0 + q4) * S::ROWS + m * 16 + c16], off, total[m], 0, 0, 0);
@@ -735,7 +730,9 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
           u32x4 xa[MT][I8 ? 2 : 4];
 #pragma unroll
           for (int m = 0; m < MT; ++m) load_rows<I8, G>(xa[m], xrow[m] + (g0 * G + s * 128) * ES, q4);
-          uint32_t dw[4] = {d.w[s][0], d.w[s][1], d.w[s][2], d.w[s][3]};
+          uint32_t dw[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dw[e] = from_lane(turn, d.w[s][e]);
           by_group<I8, G>(dw);
 #pragma unroll
           for (int g = 0; g < GS; ++g) {
@@ -743,7 +740,7 @@ __global__ __launch_bounds__(W4S_NT) void k_w4_stream(W4Args a) {
 #pragma unroll
             for (int m = 0; m < MT; ++m) r[m] = u32x4{0, 0, 0, 0};
             multiply_group<I8, G, MT>(r, xa, dw, g);
-            const float scale = I8 ? 0.0625f * sc[s * GS + g] : sc[s * GS + g];
+            const float scale = sc[s * GS + g];
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -836,16 +833,18 @@ bool streams(const W4Args& a) {
          a.lds < ((int64_t)1 << 24) && a.ldz < ((int64_t)1 << 27);
 }
 
-// Quads on their way: 4 KB of a tile and more asks for less of the code, which every launch fetches anew: shares of
-// under eight quads are done sooner with one (1 x 32000 x 4096: 18.6 us against 19.5, 8 x 4000 x 8192: 11.1 against
-// 14.2), longer ones with two (1 x 152064 x 8192: 129 us against 132).  Quads of smaller groups are shorter.
+// Quads on their way: more asks for more code, which every launch fetches anew and sixteen waves a CU execute from.
+// Groups of 64: one (16 x 128256 x 4096: 65 us against 69 with two, 1 x 32000 x 4096: 17.1 against 18.8).  Of 32, whose
+// quads are 1 KB: two (8 x 4000 x 8192: 10.9, 10.0 and 11.4 us with one, two and three; 16 x 128256 x 4096: 91, 86 and
+// 86).  Of 128: one for shares under sixteen quads (1 x 32000 x 4096: 16.9 against 18.6, 16 x 128256 x 4096: 61.6
+// against 62.8), else two (4 x 128256 x 8192: 111 against 115).
 template <bool I8, int G, int MT>
 hipError_t stream_rows(W4Args& a, hipStream_t stream) {
   if constexpr (G == 128) {
     const int64_t share = (a.N + 15) / 16 * W4StreamShape<I8, G, MT>::quads(a.K) / (W4S_WGS * W4S_WAVES);
-    return share < 8 ? launch_stream<I8, G, MT, 1>(a, stream) : launch_stream<I8, G, MT, 2>(a, stream);
+    return share < 16 ? launch_stream<I8, G, MT, 1>(a, stream) : launch_stream<I8, G, MT, 2>(a, stream);
   } else {
-    return launch_stream<I8, G, MT, G == 64 ? 2 : 3>(a, stream);
+    return launch_stream<I8, G, MT, G == 64 ? 1 : 2>(a, stream);
   }
 }
 
