@@ -186,3 +186,19 @@ def test_repeatable_on_another_stream_and_empty():
             s.synchronize()
             assert torch.equal(a, b)
     assert alb.matmul_w4(torch.empty((0, 1024), dtype=torch.bfloat16, device="cuda"), w).shape == (0, 3000)
+
+
+@pytest.mark.parametrize("K", [384, 512, 640, 896, 1152])
+@pytest.mark.parametrize("B,N", [(64, 9001), (66, 49300)])
+def test_groups_that_end_inside_a_load_of_scales(B, N, K):
+    """8-bit rows and groups of 128 in weights wide enough for whole rounds of workgroups: 3 to 9 groups a row."""
+    import torch
+
+    import paper_2606_01927_amd as alb
+
+    rng = np.random.default_rng(B + N + K)
+    for zeros, sdt, pad in ((False, torch.bfloat16, 0), (True, torch.float32, 1), (True, torch.bfloat16, 0), (False, torch.float32, 1)):
+        w, dense, _ = _weights(rng, N, K, 128, zeros, True, sdt, pad if sdt == torch.float32 else 0)
+        x, sc = _rows_in(rng, B, K, True, True)
+        got = alb.matmul_w4(x, w, x_scale=sc).double().cpu().numpy()
+        assert np.array_equal(got, _dense_x(x, sc) @ dense.T), (zeros, sdt, pad)
